@@ -186,6 +186,107 @@ int vpe_encode(vpe_engine* e, const float* images, void* stream, vpe_feat* out);
 int vpe_preprocess_u8(const uint8_t* frames, int batch, int src_h, int src_w, float* images, int dst_h, int dst_w,
                       const float mean[3], const float std[3], void* stream);
 
+/* ---- Operators for packed requests ----
+ * Rows of many requests -- views of different sizes, tokens of different streams -- lie behind one another in one matrix, and
+ * each call below works on all of them.  Like vpe_preprocess_u8 they need no engine: the caller owns every buffer (DEVICE
+ * memory on the current device unless stated otherwise), calls only enqueue (stream NULL = the default stream), nothing is
+ * allocated, and they may be captured into a graph.  What a struct's arrays hold on the device is read when the work runs, so a
+ * captured call follows them from replay to replay; sizes, flags and pointers are those of the call.  A workspace belongs to a
+ * call until its work is done: calls that may overlap need one each.  Inputs may not overlap outputs (vpe_block_norm's x and out may be one
+ * buffer).  They return VPE_EINVAL (vpe_last_error(NULL) says why; nothing has been enqueued) or VPE_EHIP. */
+
+/* Attention over packed sequences, each against keys of its own: out = softmax(score) v, per head.
+ *   Sequence s has the query rows q_offsets[s] .. q_offsets[s + 1] - 1 (nq of them) and the key rows k_offsets[s] .. (nk of
+ *   them: k_lengths[s], or up to k_offsets[s + 1] where k_lengths is null).  Query head h reads key head h / (heads / kv_heads).
+ *   Query row i stands at place i + nk - nq (the last query at the last key) and key j at place j.
+ *     score = scale q.k;  cap > 0: cap tanh(score / cap);  then, with slopes, minus slopes[h] * distance: the difference of the
+ *     two places, or with coordinates the Euclidean distance of q_coords[row] and k_coords[row] (fp32 pairs by row of q and k).
+ *     causal = 0: every key is seen;  1: key j is seen from places j and up, and from everywhere if j < prefix[s] (null: 0).
+ *   A row that sees no key, or whose scores are all -inf, is zero, its lse -inf.  Keys that a row does not see do not enter its
+ *   result, whatever they hold.  lse (may be null): natural logarithm of the sum of exp(score), fp32 [q_rows][heads].
+ *   Rows of out and lse that belong to no sequence keep their contents.
+ *   Single tokens against a cache are sequences of one query row; k_offsets then are the places of the cache's slots.
+ *   max_q, max_k: upper bounds of nq and nk (queries and keys beyond them are left out); they set the grid and the split of
+ *   the keys, so tight ones are faster.  Offsets that are negative, decreasing or past q_rows / k_rows are cut to the rows there are.
+ *   Scores and sums are fp32; bf16 calls round the probabilities to bf16 for the product with v, the sum takes them unrounded.
+ * Limits: head_dim 64 or 128, heads a multiple of kv_heads; q, k, v, out 16-byte aligned, their strides (in elements) of rows
+ * and heads multiples of 16 bytes and not negative, last axis contiguous, out's at least head_dim. */
+typedef struct {
+    int32_t dtype;                    /* vpe_dtype of q, k, v and out */
+    int32_t heads, kv_heads, head_dim;
+    int32_t sequences, max_q, max_k;
+    int32_t q_rows, k_rows;           /* rows that q / out / lse / q_coords and k / v / k_coords have */
+    int32_t causal;
+    float   scale, cap;               /* finite; cap >= 0 (0: none) */
+    const void *q, *k, *v;
+    void* out;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;   /* strides in elements */
+    const int32_t *q_offsets, *k_offsets;   /* [sequences + 1] */
+    const int32_t *k_lengths, *prefix;      /* [sequences] or null */
+    const float* slopes;              /* [heads] or null */
+    const float *q_coords, *k_coords; /* [rows][2], both or neither, with slopes */
+    float* lse;
+    void* workspace;                  /* 256-byte aligned; may be null where vpe_attention_workspace_bytes says 0 */
+    uint64_t workspace_bytes;
+} vpe_attention_args;
+/* Workspace of a call: depends on the sizes alone (dtype .. k_rows of the struct; pointers are not looked at). */
+int vpe_attention_workspace_bytes(const vpe_attention_args* args, uint64_t* bytes);
+int vpe_attention(const vpe_attention_args* args, void* stream);
+
+/* What stands between two blocks, in one pass over the rows (row r of request request[r]):
+ *     y   = post-norm of branch (gain post_gain, bias post_bias), times layer_scale, times gate[request]
+ *     out = residual_scale x + y                                   fp32; out may be x
+ *     normed = pre-norm of out (pre_gain, pre_bias), times 1 + scale[request], plus shift[request]     dtype
+ *   A norm is VPE_NORM_LAYER (biased variance), VPE_NORM_RMS or VPE_NORM_NONE (the values themselves; gain and bias are not
+ *   read then), eps inside the root; statistics in fp32, mean first.  Null: gain 1, bias 0, layer_scale 1, gate 1, scale 0,
+ *   shift 0; branch null: y = 0 (the norm in front of the first block); normed null: not written (behind the last one).
+ *   request null: all rows are of request 0; rows with an index outside 0 .. requests - 1 have gate 1, scale 0 and shift 0.
+ * Limits: dim up to 8192; rows contiguous at any alignment of their type, row strides in elements at least dim. */
+typedef enum { VPE_NORM_NONE = 0, VPE_NORM_LAYER = 1, VPE_NORM_RMS = 2 } vpe_norm;
+typedef struct {
+    int32_t dtype;                    /* vpe_dtype of branch and normed */
+    int32_t rows, dim, requests;
+    int32_t post, pre;                /* vpe_norm */
+    float   residual_scale, eps;      /* finite; eps > 0 */
+    const float* x;
+    const void* branch;
+    float* out;
+    void* normed;
+    int64_t x_row, branch_row, out_row, normed_row;   /* strides in elements */
+    const float *post_gain, *post_bias, *pre_gain, *pre_bias, *layer_scale;   /* [dim] or null */
+    const float *gate, *scale, *shift;                /* [requests][dim] or null */
+    const int32_t* request;           /* [rows] or null */
+} vpe_block_norm_args;
+int vpe_block_norm(const vpe_block_norm_args* args, void* stream);
+
+/* A projection that all rows share, and beside it the low-rank adapter of each row:
+ *     out[r] = x[r] weight^T + bias + scale[a] (x[r] A[a]^T) B[a]^T,   a = adapter[r]
+ *   weight [out_features][in_features], A [adapters][rank][in_features], B [adapters][out_features][rank], all in dtype and
+ *   contiguous; bias fp32 [out_features] or null; scale fp32 [adapters] or null (1); adapter [rows] or null (rows have none);
+ *   rows whose index lies outside 0 .. adapters - 1 have none.  Rows may come in any order; rows of one adapter that lie
+ *   together share its reads.  Sums are fp32; bf16 calls carry x A^T to the second product in two bf16 terms (16 bits).
+ * Limits: in_features a multiple of 64, rank a multiple of 8 up to 128 (fewer: zero rows and columns do not change the result);
+ * x, weight, A and B 16-byte aligned, x's row stride a multiple of 16 bytes and at least in_features; out's row stride at least
+ * out_features. */
+typedef struct {
+    int32_t dtype;                    /* vpe_dtype of x, weight, a, b and (out_f32 = 0) out */
+    int32_t out_f32;                  /* 1: out is fp32 */
+    int32_t rows, in_features, out_features;
+    int32_t adapters, rank;           /* adapters 0: a, b, adapter and scale are not looked at */
+    const void *x, *weight;
+    const float* bias;
+    void* out;
+    int64_t x_row, out_row;           /* strides in elements */
+    const void *a, *b;
+    const int32_t* adapter;
+    const float* scale;
+    void* workspace;                  /* 256-byte aligned; may be null where vpe_adapter_linear_workspace_bytes says 0 */
+    uint64_t workspace_bytes;
+} vpe_adapter_linear_args;
+/* Workspace of a call: depends on the sizes alone (dtype .. rank of the struct; pointers are not looked at). */
+int vpe_adapter_linear_workspace_bytes(const vpe_adapter_linear_args* args, uint64_t* bytes);
+int vpe_adapter_linear(const vpe_adapter_linear_args* args, void* stream);
+
 /* The engine-owned stream that the next vpe_encode / vpe_encode_at with stream == NULL will run on (one per
  * encoder lane, taken in turn).  Work the caller enqueues on it first -- vpe_preprocess_u8, a host-to-device
  * copy of the frame -- is ordered before that encode without an event and without another stream competing

@@ -16,6 +16,7 @@ VPE_OK, VPE_SKIPPED, VPE_BUSY, VPE_EINVAL, VPE_ENOMEM, VPE_ESTALE, VPE_EHIP = 0,
 VPE_F32, VPE_BF16 = 0, 1
 VPE_MLP_GELU, VPE_MLP_SWIGLU = 0, 1
 VPE_HEAD_SEG, VPE_HEAD_DEPTH, VPE_HEAD_DET, VPE_HEAD_DPT = 0, 1, 2, 3
+VPE_NORM_NONE, VPE_NORM_LAYER, VPE_NORM_RMS = 0, 1, 2
 VPE_FLAG_GRAPHS, VPE_FLAG_HOST_ONLY, VPE_FLAG_WALL_CLOCK, VPE_FLAG_TIMING = 1, 2, 4, 8
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -39,6 +40,26 @@ class vpe_backbone_cfg(C.Structure):
 class vpe_head_cfg(C.Structure):
     _fields_ = [("kind", C.c_int32), ("classes", C.c_int32), ("channels", C.c_int32), ("every_n", C.c_int32),
                 ("weights", C.c_void_p), ("weights_bytes", C.c_uint64)]
+
+
+class vpe_attention_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "heads", "kv_heads", "head_dim", "sequences", "max_q", "max_k", "q_rows", "k_rows", "causal")] + \
+               [("scale", C.c_float), ("cap", C.c_float)] + [(n, C.c_void_p) for n in ("q", "k", "v", "out")] + \
+               [(n, C.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "out_row", "out_head")] + \
+               [(n, C.c_void_p) for n in ("q_offsets", "k_offsets", "k_lengths", "prefix", "slopes", "q_coords", "k_coords", "lse", "workspace")] + \
+               [("workspace_bytes", C.c_uint64)]
+
+
+class vpe_block_norm_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "rows", "dim", "requests", "post", "pre")] + [("residual_scale", C.c_float), ("eps", C.c_float)] + \
+               [(n, C.c_void_p) for n in ("x", "branch", "out", "normed")] + [(n, C.c_int64) for n in ("x_row", "branch_row", "out_row", "normed_row")] + \
+               [(n, C.c_void_p) for n in ("post_gain", "post_bias", "pre_gain", "pre_bias", "layer_scale", "gate", "scale", "shift", "request")]
+
+
+class vpe_adapter_linear_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "out_f32", "rows", "in_features", "out_features", "adapters", "rank")] + \
+               [(n, C.c_void_p) for n in ("x", "weight", "bias", "out")] + [(n, C.c_int64) for n in ("x_row", "out_row")] + \
+               [(n, C.c_void_p) for n in ("a", "b", "adapter", "scale", "workspace")] + [("workspace_bytes", C.c_uint64)]
 
 
 class VpeError(RuntimeError):
@@ -79,12 +100,18 @@ def load_library(path: Optional[str] = None):
     L.vpe_stage_times.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(C.c_float), i32]
     L.vpe_stats.argtypes = [vp, i64p, i64p, i64p, i32]
     L.vpe_time_kernel.argtypes = [vp, i32, i32, C.POINTER(C.c_float), C.POINTER(C.c_double), C.POINTER(C.c_double)]
+    L.vpe_attention_workspace_bytes.argtypes = [C.POINTER(vpe_attention_args), C.POINTER(C.c_uint64)]
+    L.vpe_attention.argtypes = [C.POINTER(vpe_attention_args), vp]
+    L.vpe_block_norm.argtypes = [C.POINTER(vpe_block_norm_args), vp]
+    L.vpe_adapter_linear_workspace_bytes.argtypes = [C.POINTER(vpe_adapter_linear_args), C.POINTER(C.c_uint64)]
+    L.vpe_adapter_linear.argtypes = [C.POINTER(vpe_adapter_linear_args), vp]
     L.vpe_last_error.argtypes = [vp]
     L.vpe_last_error.restype = C.c_char_p
     L.vpe_destroy.argtypes = [vp]
     L.vpe_destroy.restype = None
     for n in ("vpe_workspace_bytes", "vpe_create", "vpe_encode", "vpe_encode_at", "vpe_run_head", "vpe_set_head_rate",
-              "vpe_set_head_rate_hz", "vpe_preprocess_u8", "vpe_next_encode_stream", "vpe_feat_view",
+              "vpe_set_head_rate_hz", "vpe_preprocess_u8", "vpe_attention_workspace_bytes", "vpe_attention", "vpe_block_norm",
+              "vpe_adapter_linear_workspace_bytes", "vpe_adapter_linear", "vpe_next_encode_stream", "vpe_feat_view",
               "vpe_head_output", "vpe_sync", "vpe_run_head_static", "vpe_head_done", "vpe_wait_head", "vpe_stage_times", "vpe_stats", "vpe_time_kernel", "vpe_run_head_latest", "vpe_head_counters", "vpe_frame_ready"):
         getattr(L, n).restype = C.c_int
     if path is None:
@@ -143,6 +170,186 @@ def preprocess_u8(frames, out, mean, std, stream=None) -> None:
     vpe_preprocess_u8(frames.data_ptr(), frames.shape[0], frames.shape[1], frames.shape[2], out.data_ptr(),
                       out.shape[2], out.shape[3], mean, std,
                       None if stream is None else stream if isinstance(stream, int) else stream.cuda_stream)
+
+
+# ------------------------------------------------------------------ operators on packed rows
+def _raw_stream(stream) -> Optional[int]:
+    """A torch stream, a raw hipStream_t as int, or None (the default stream)."""
+    return None if stream is None else stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _dtype_of(t) -> int:
+    import torch
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise VpeError(VPE_EINVAL, f"tensors must be bfloat16 or float32, not {t.dtype}")
+    return VPE_BF16 if t.dtype == torch.bfloat16 else VPE_F32
+
+
+def _device_ptr(name: str, t, device, dtype=None, shape=None, contiguous=True) -> Optional[int]:
+    """The address of a tensor that a call is to use, or None for None; what does not fit is refused."""
+    if t is None:
+        return None
+    if dtype is not None and t.dtype != dtype:
+        raise VpeError(VPE_EINVAL, f"{name} must be {dtype}, not {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise VpeError(VPE_EINVAL, f"{name} has the shape {tuple(t.shape)}, {tuple(shape)} expected")
+    if contiguous and not t.is_contiguous():
+        raise VpeError(VPE_EINVAL, f"{name} must be contiguous")
+    if t.device != device:
+        raise VpeError(VPE_EINVAL, f"{name} is on {t.device}, {device} expected")
+    return t.data_ptr()
+
+
+def _workspace(args, workspace, device) -> None:
+    import torch
+    if workspace is None:
+        return
+    if workspace.dtype != torch.uint8:
+        raise VpeError(VPE_EINVAL, "workspace must be a uint8 tensor")
+    args.workspace = _device_ptr("workspace", workspace, device)
+    args.workspace_bytes = workspace.numel()
+
+
+def _enqueue(call, args, device, stream) -> None:
+    """Makes the call with the tensors' device current."""
+    import torch
+    if device.type != "cuda":
+        raise VpeError(VPE_EINVAL, f"tensors are on {device}: device memory required")
+    with torch.cuda.device(device):
+        rc = call(C.byref(args), _raw_stream(stream))
+    if rc:
+        raise VpeError(rc, vpe_last_error(None))
+
+
+def _row_stride(name: str, t) -> int:
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise VpeError(VPE_EINVAL, f"{name} must be a matrix with contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])      # (the stride of a single row says nothing)
+
+
+def _attention_sizes(q, k, sequences: int, max_q: int, max_k: int) -> vpe_attention_args:
+    if q.dim() != 3 or k.dim() != 3 or q.shape[2] != k.shape[2] or q.dtype != k.dtype:
+        raise VpeError(VPE_EINVAL, "q and k must be [rows, heads, head_dim] of one type and head_dim")
+    a = vpe_attention_args()
+    a.dtype, a.heads, a.kv_heads, a.head_dim = _dtype_of(q), q.shape[1], k.shape[1], q.shape[2]
+    a.sequences, a.max_q, a.max_k, a.q_rows, a.k_rows = sequences, max_q, max_k, q.shape[0], k.shape[0]
+    return a
+
+
+def attention_workspace_bytes(q, k, *, sequences: int, max_q: int, max_k: int) -> int:
+    """Bytes of workspace that `attention` needs for tensors of these shapes, whatever the offsets say."""
+    a, out = _attention_sizes(q, k, sequences, max_q, max_k), C.c_uint64(0)
+    rc = lib().vpe_attention_workspace_bytes(C.byref(a), C.byref(out))
+    if rc:
+        raise VpeError(rc, vpe_last_error(None))
+    return int(out.value)
+
+
+def attention(q, k, v, out, *, q_offsets, k_offsets, max_q: int, max_k: int, k_lengths=None, causal: bool = False, prefix=None,
+              scale: Optional[float] = None, cap: float = 0.0, slopes=None, q_coords=None, k_coords=None, lse=None, workspace=None,
+              stream=None) -> None:
+    """vpe_attention on torch CUDA tensors: q, out [q_rows, heads, head_dim], k, v [k_rows, kv_heads, head_dim] (rows and heads of any
+    stride, last axis contiguous; bfloat16 or float32); q_offsets, k_offsets int32 [sequences + 1], k_lengths, prefix int32
+    [sequences]; slopes float32 [heads]; coordinates float32 [rows, 2]; lse float32 [q_rows, heads] (written, as is out).
+    scale: 1 / sqrt(head_dim) if not given.  workspace: a uint8 tensor of attention_workspace_bytes.  stream: a torch stream, a raw
+    hipStream_t as int, or None (the default stream)."""
+    import torch
+    sequences = q_offsets.numel() - 1
+    a = _attention_sizes(q, k, sequences, max_q, max_k)
+    dev, heads = q.device, a.heads
+    if v.shape != k.shape or out.shape != q.shape:
+        raise VpeError(VPE_EINVAL, "v must have k's shape, out q's")
+    for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
+        if t.stride(2) != 1 and t.numel():
+            raise VpeError(VPE_EINVAL, f"{name}'s last axis must be contiguous")
+        setattr(a, name, _device_ptr(name, t, dev, q.dtype, contiguous=False))
+        # (the stride of an axis of length one says nothing)
+        setattr(a, name + "_row", t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2])
+        setattr(a, name + "_head", t.stride(1) if t.shape[1] > 1 else t.shape[2])
+    a.causal, a.scale, a.cap = int(bool(causal)), q.shape[2] ** -0.5 if scale is None else scale, cap
+    i32, f32 = torch.int32, torch.float32
+    a.q_offsets = _device_ptr("q_offsets", q_offsets, dev, i32, (sequences + 1,))
+    a.k_offsets = _device_ptr("k_offsets", k_offsets, dev, i32, (sequences + 1,))
+    a.k_lengths = _device_ptr("k_lengths", k_lengths, dev, i32, (sequences,))
+    a.prefix = _device_ptr("prefix", prefix, dev, i32, (sequences,))
+    a.slopes = _device_ptr("slopes", slopes, dev, f32, (heads,))
+    a.q_coords = _device_ptr("q_coords", q_coords, dev, f32, (q.shape[0], 2))
+    a.k_coords = _device_ptr("k_coords", k_coords, dev, f32, (k.shape[0], 2))
+    a.lse = _device_ptr("lse", lse, dev, f32, (q.shape[0], heads))
+    _workspace(a, workspace, dev)
+    _enqueue(lib().vpe_attention, a, dev, stream)
+
+
+def block_norm(x, out, *, branch=None, normed=None, post: int = VPE_NORM_NONE, post_gain=None, post_bias=None, pre: int = VPE_NORM_NONE,
+               pre_gain=None, pre_bias=None, layer_scale=None, residual_scale: float = 1.0, gate=None, scale=None, shift=None,
+               request=None, eps: float = 1e-6, stream=None) -> None:
+    """vpe_block_norm on torch CUDA tensors: x, out float32 [rows, dim] (out is written and may be x); branch, normed [rows, dim],
+    bfloat16 or float32 (normed is written); gains, biases and layer_scale float32 [dim]; gate, scale, shift float32 [requests, dim];
+    request int32 [rows].  Rows may be strided.  stream: as for attention."""
+    import torch
+    a, dev, (rows, dim) = vpe_block_norm_args(), x.device, x.shape
+    typed = [t for t in (branch, normed) if t is not None]
+    a.dtype = _dtype_of(typed[0]) if typed else VPE_F32
+    for name, t, dtype in (("x", x, torch.float32), ("out", out, torch.float32), ("branch", branch, None), ("normed", normed, None)):
+        if t is None:
+            continue
+        setattr(a, name, _device_ptr(name, t, dev, dtype or typed[0].dtype, (rows, dim), contiguous=False))
+        setattr(a, name + "_row", _row_stride(name, t))
+    modulation = [t for t in (gate, scale, shift) if t is not None]
+    a.rows, a.dim, a.requests = rows, dim, modulation[0].shape[0] if modulation else 0
+    a.post, a.pre, a.residual_scale, a.eps = post, pre, residual_scale, eps
+    for name, t in (("post_gain", post_gain), ("post_bias", post_bias), ("pre_gain", pre_gain), ("pre_bias", pre_bias), ("layer_scale", layer_scale)):
+        setattr(a, name, _device_ptr(name, t, dev, torch.float32, (dim,)))
+    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
+        setattr(a, name, _device_ptr(name, t, dev, torch.float32, (a.requests, dim)))
+    a.request = _device_ptr("request", request, dev, torch.int32, (rows,))
+    _enqueue(lib().vpe_block_norm, a, dev, stream)
+
+
+def _adapter_sizes(x, weight, a_) -> vpe_adapter_linear_args:
+    if x.dim() != 2 or weight.dim() != 2 or x.shape[1] != weight.shape[1] or x.dtype != weight.dtype:
+        raise VpeError(VPE_EINVAL, "x must be [rows, in_features], weight [out_features, in_features] of one type")
+    p = vpe_adapter_linear_args()
+    p.dtype, p.rows, p.in_features, p.out_features = _dtype_of(x), x.shape[0], x.shape[1], weight.shape[0]
+    if a_ is not None:
+        if a_.dim() != 3 or a_.shape[2] != x.shape[1]:
+            raise VpeError(VPE_EINVAL, "a must be [adapters, rank, in_features]")
+        p.adapters, p.rank = a_.shape[0], a_.shape[1]
+    return p
+
+
+def adapter_linear_workspace_bytes(x, weight, a=None) -> int:
+    """Bytes of workspace that `adapter_linear` needs for tensors of these shapes."""
+    p, out = _adapter_sizes(x, weight, a), C.c_uint64(0)
+    rc = lib().vpe_adapter_linear_workspace_bytes(C.byref(p), C.byref(out))
+    if rc:
+        raise VpeError(rc, vpe_last_error(None))
+    return int(out.value)
+
+
+def adapter_linear(x, weight, out, *, bias=None, a=None, b=None, adapter=None, scale=None, workspace=None, stream=None) -> None:
+    """vpe_adapter_linear on torch CUDA tensors: x [rows, in_features] (rows may be strided), weight [out_features, in_features],
+    a [adapters, rank, in_features], b [adapters, out_features, rank], all bfloat16 or all float32; out [rows, out_features] of
+    that type or float32 (written); bias float32 [out_features]; adapter int32 [rows] (outside 0 .. adapters - 1: none); scale float32
+    [adapters].  workspace: a uint8 tensor of adapter_linear_workspace_bytes.  stream: as for attention."""
+    import torch
+    p, dev = _adapter_sizes(x, weight, a), x.device
+    if (a is None) != (b is None) or (a is None) != (adapter is None):
+        raise VpeError(VPE_EINVAL, "a, b and adapter go together")
+    if out.dtype not in (x.dtype, torch.float32):
+        raise VpeError(VPE_EINVAL, f"out must be {x.dtype} or float32, not {out.dtype}")
+    p.out_f32 = int(out.dtype == torch.float32)
+    p.x = _device_ptr("x", x, dev, contiguous=False)
+    p.out = _device_ptr("out", out, dev, shape=(x.shape[0], weight.shape[0]), contiguous=False)
+    p.x_row, p.out_row = _row_stride("x", x), _row_stride("out", out)
+    p.weight = _device_ptr("weight", weight, dev)
+    p.bias = _device_ptr("bias", bias, dev, torch.float32, (weight.shape[0],))
+    p.a = _device_ptr("a", a, dev, x.dtype)
+    p.b = _device_ptr("b", b, dev, x.dtype, (p.adapters, weight.shape[0], p.rank))
+    p.adapter = _device_ptr("adapter", adapter, dev, torch.int32, (x.shape[0],))
+    p.scale = _device_ptr("scale", scale, dev, torch.float32, (p.adapters,))
+    _workspace(p, workspace, dev)
+    _enqueue(lib().vpe_adapter_linear, p, dev, stream)
 
 
 def vpe_next_encode_stream(engine) -> Optional[int]:

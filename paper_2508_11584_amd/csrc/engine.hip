@@ -19,6 +19,7 @@
 #include <vector>
 
 #include "kernels.h"
+#include "operators.h"
 #include "vpe.h"
 
 using namespace vpe;
@@ -997,6 +998,11 @@ void destroy_engine(vpe_engine* e) {
 }
 
 }  // namespace
+
+int vpe::call_error(int code, const char* message) noexcept {
+    try { g_create_error = message; } catch (...) { g_create_error.clear(); }
+    return code;
+}
 
 // ====================================================================== C ABI
 extern "C" {

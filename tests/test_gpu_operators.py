@@ -1,0 +1,657 @@
+"""The operators on packed rows against their definitions in 64 bits.
+
+Tolerances are sums of roundings.  u = 2^-24 is half a step of fp32 relative to the value, 2^-8 half a step of bf16.  The error of a
+sum of n terms in fp32 is taken as (4 sqrt(n) + 16) u times the sum of the terms' magnitudes: its n roundings are independent and add
+up like a random walk (four deviations), a handful of further operations come with it.
+"""
+import math
+
+import pytest
+import torch
+
+import paper_2508_11584_amd as vpe
+
+pytestmark = pytest.mark.gpu
+
+U, HALF_BF16 = 2.0 ** -24, 2.0 ** -8
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def walk(n):
+    return (4.0 * math.sqrt(n) + 16.0) * U
+
+
+def normal(gen, shape, std=1.0, dtype=torch.float32):
+    return (std * torch.randn(shape, generator=gen)).to("cuda", dtype)
+
+
+def i32(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def held(got, ref, tol, what=""):
+    """Every element within its tolerance; NaN and infinities where the definition has them."""
+    got, ref = got.double(), ref.double()
+    assert got.shape == ref.shape
+    same = (got == ref) | (got.isnan() & ref.isnan())
+    bad = ~same & ~((got - ref).abs() <= tol)
+    if bool(bad.any()):
+        at = tuple(int(v) for v in torch.nonzero(bad)[0])
+        t = tol[at] if torch.is_tensor(tol) else tol
+        raise AssertionError(f"{what}: {int(bad.sum())} of {bad.numel()} outside, first at {at}: {float(got[at])} for {float(ref[at])}, tolerance {float(t)}")
+
+
+# ------------------------------------------------------------------ attention
+def attention_f64(q, k, v, q_at, ks, k_at, *, causal=False, prefix=None, scale=None, cap=0.0, slopes=None, coords=None):
+    """Result and lse in 64 bits, and the tolerance of each for fp32 arithmetic without the rounding of the result.  NaN for rows of no sequence."""
+    H, D, G = q.shape[1], q.shape[2], q.shape[1] // k.shape[1]
+    out = torch.full(q.shape, math.nan, dtype=torch.float64, device="cuda")
+    lse = torch.full(q.shape[:2], math.nan, dtype=torch.float64, device="cuda")
+    mag, tol_p, tol_l = out.clone(), lse.clone(), lse.clone()
+    scale = D ** -0.5 if scale is None else scale
+    for s, nk in enumerate(ks):
+        q0, nq, k0 = q_at[s], q_at[s + 1] - q_at[s], k_at[s]
+        for h in range(H):
+            a, b, w = q[q0:q0 + nq, h].double(), k[k0:k0 + nk, h // G].double(), v[k0:k0 + nk, h // G].double()
+            x = a @ b.t().contiguous() * scale
+            err = (a.abs() @ b.abs().t().contiguous()) * abs(scale) * walk(D)
+            if cap:
+                x = cap * torch.tanh(x / cap)
+                err = err + 8.0 * U * cap
+            place = torch.arange(nq, device="cuda").view(-1, 1) + (nk - nq)
+            key = torch.arange(nk, device="cuda")
+            if slopes is not None:
+                if coords is not None:
+                    dist = torch.cdist(coords[0][q0:q0 + nq].double(), coords[1][k0:k0 + nk].double(), compute_mode="donot_use_mm_for_euclid_dist")
+                else:
+                    dist = (place - key).abs().double()
+                x = x - slopes[h].double() * dist
+                err = err + 8.0 * U * slopes[h].double().abs() * dist
+            err = err + 8.0 * U * x.abs()
+            seen = torch.ones_like(x, dtype=torch.bool)
+            if causal:
+                seen = (key <= place) | (key < (prefix[s] if prefix else 0))
+            x = torch.where(seen, x, torch.full_like(x, -math.inf))
+            err = torch.where(seen, err, torch.zeros_like(err))
+            e_row = torch.nan_to_num(err, nan=0.0, posinf=0.0).amax(1) if nk else torch.zeros(nq, dtype=torch.float64, device="cuda")
+            any_ = (x > -math.inf).any(1) | x.isnan().any(1) if nk else torch.zeros(nq, dtype=torch.bool, device="cuda")
+            top = torch.where(any_, x.amax(1), torch.zeros_like(e_row)) if nk else e_row
+            p = torch.where(seen, torch.exp(x - top.view(-1, 1)), torch.zeros_like(x))
+            total = p.sum(1)
+            w_seen = torch.where(p.isnan() | (p > 0), 1.0, 0.0)
+            finite = bool(torch.isfinite(w).all())
+            if finite:
+                o, m = p @ w, p @ w.abs()
+            else:                                      # a value that no row weighs must not count: no 0 x NaN
+                o, m = torch.zeros((nq, D), dtype=torch.float64, device="cuda"), None
+                for j in range(nk):
+                    o = o + torch.where(seen[:, j:j + 1], p[:, j:j + 1] * w[j], torch.zeros_like(o))
+                m = torch.nan_to_num(o.abs(), nan=0.0, posinf=0.0)
+            safe = torch.where(any_, total, torch.ones_like(total)).view(-1, 1)
+            out[q0:q0 + nq, h] = torch.where(any_.view(-1, 1), o / safe, torch.zeros_like(o))
+            mag[q0:q0 + nq, h] = torch.where(any_.view(-1, 1), m / safe, torch.zeros_like(o))
+            lse[q0:q0 + nq, h] = torch.where(any_, top + torch.log(safe[:, 0]), torch.full_like(top, -math.inf))
+            del w_seen
+            tol_p[q0:q0 + nq, h] = 2.0 * e_row + 2.0 * walk(nk)
+            tol_l[q0:q0 + nq, h] = e_row + walk(nk) + 4.0 * U * lse[q0:q0 + nq, h].abs().nan_to_num(posinf=0.0)
+    return out, lse, mag, tol_p, tol_l
+
+
+def places(lengths):
+    at = [0]
+    for n in lengths:
+        at.append(at[-1] + n)
+    return at
+
+
+def run_attention(q, k, v, q_at, ks, k_at, *, packed, dtype, max_q=None, max_k=None, out=None, stream=None, workspace=None, **kw):
+    out = torch.full_like(q, 7.0).contiguous() if out is None else out
+    lse = torch.full(q.shape[:2], 7.0, device="cuda")
+    mq = max([b - a for a, b in zip(q_at, q_at[1:])], default=0) if max_q is None else max_q
+    mk = max(ks, default=0) if max_k is None else max_k
+    if workspace is None:
+        need = vpe.attention_workspace_bytes(q, k, sequences=len(ks), max_q=mq, max_k=mk)
+        workspace = torch.full((need,), 255, dtype=torch.uint8, device="cuda") if need else None
+    coords = kw.pop("coords", None)
+    vpe.attention(q, k, v, out, q_offsets=i32(q_at), k_offsets=i32(k_at if len(k_at) == len(ks) + 1 else list(k_at) + [k.shape[0]]),
+                  k_lengths=None if packed else i32(ks), max_q=mq, max_k=mk, lse=lse, workspace=workspace, stream=stream,
+                  prefix=i32(kw.pop("prefix")) if kw.get("prefix") else kw.pop("prefix", None) and None,
+                  q_coords=coords[0] if coords else None, k_coords=coords[1] if coords else None, **kw)
+    return out, lse
+
+
+def check_attention(q, k, v, q_at, ks, k_at, *, packed=True, dtype="bf16", **kw):
+    out, lse = run_attention(q, k, v, q_at, ks, k_at, packed=packed, dtype=dtype, **dict(kw))
+    ref, ref_l, mag, tol_p, tol_l = attention_f64(q, k, v, q_at, ks, k_at, **kw)
+    torch.cuda.synchronize()
+    half = HALF_BF16 if dtype == "bf16" else U
+    # probabilities rounded to bf16 weigh the values (half a step of each), the result is rounded once
+    tol = (tol_p.unsqueeze(2) + (HALF_BF16 if dtype == "bf16" else 0.0)) * mag + half * ref.abs() + 1e-30
+    n = q_at[-1]
+    held(out[:n], ref[:n], tol[:n], "out")
+    held(lse[:n], ref_l[:n], tol_l[:n], "lse")
+    assert bool((out[n:] == 7.0).all()) and bool((lse[n:] == 7.0).all()), "rows of no sequence were written"
+    return out, lse
+
+
+FORMS = {
+    "one": dict(qs=[1], ks=[1]), "short": dict(qs=[3, 1, 5], ks=[3, 1, 5]), "empty_sequences": dict(qs=[0, 17, 0, 2, 0], ks=[5, 40, 0, 2, 9]),
+    "no_keys": dict(qs=[4, 3], ks=[0, 7]), "views": dict(qs=[257, 64, 130, 1], ks=[257, 64, 130, 1]), "odd": dict(qs=[127, 129], ks=[65, 191]),
+    "causal": dict(qs=[200, 31], ks=[200, 31], causal=True), "causal_tail": dict(qs=[33, 7], ks=[300, 129], causal=True),
+    "rows_without_keys": dict(qs=[150, 9], ks=[70, 3], causal=True), "prefix": dict(qs=[140, 90, 33], ks=[140, 90, 33], causal=True, prefix=[50, 0, 999]),
+    "prefix_before_rows": dict(qs=[100, 5], ks=[60, 2], causal=True, prefix=[20, -4]), "capped": dict(qs=[190], ks=[190], cap=5.0),
+    "line": dict(qs=[150, 20], ks=[150, 70], slopes=True), "grid": dict(qs=[131, 77], ks=[131, 77], slopes=True, coords=True),
+    "all": dict(qs=[100, 66], ks=[160, 66], causal=True, prefix=[30, 8], cap=20.0, slopes=True), "token": dict(qs=[1, 1, 1], ks=[1000, 1, 64], causal=True),
+    "token_capped": dict(qs=[1, 2], ks=[700, 300], causal=True, cap=10.0, slopes=True), "token_long": dict(qs=[1], ks=[9001], causal=True),
+    "tokens_uneven": dict(qs=[1, 0, 3, 1], ks=[5000, 77, 2049, 0], causal=True), "long": dict(qs=[1500], ks=[1500]),
+}
+HEADS = [(1, 1, 64), (6, 6, 64), (8, 2, 64), (4, 4, 128), (12, 1, 128)]
+
+
+def attention_case(form, heads, kv_heads, head_dim, dtype, seed=0, spread=1.6, extra=5):
+    f = dict(FORMS[form])
+    qs, ks = f.pop("qs"), f.pop("ks")
+    gen = torch.Generator().manual_seed(100 + seed)
+    q_at, k_at, T = places(qs), places(ks), DTYPES[dtype]
+    q = normal(gen, (q_at[-1] + extra, heads, head_dim), spread, T)
+    k, v = (normal(gen, (k_at[-1] + extra, kv_heads, head_dim), spread, T) for _ in range(2))
+    if f.pop("slopes", False):
+        f["slopes"] = torch.exp2(-8.0 * torch.arange(1, heads + 1) / heads).cuda()
+    if f.pop("coords", False):
+        f["coords"] = (normal(gen, (q.shape[0], 2), 9.0), normal(gen, (k.shape[0], 2), 9.0))
+    return q, k, v, q_at, ks, k_at, f
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_attention_against_its_definition(form, dtype):
+    for n, (h, kh, d) in enumerate(HEADS if form in ("views", "all", "token", "causal_tail", "token_capped") else HEADS[2:4]):
+        q, k, v, q_at, ks, k_at, kw = attention_case(form, h, kh, d, dtype, seed=n)
+        check_attention(q, k, v, q_at, ks, k_at, dtype=dtype, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["rows_of_qkv", "heads_first", "slots", "broadcast_value"])
+def test_attention_reads_strided_tensors(layout, dtype):
+    gen, T = torch.Generator().manual_seed(5), DTYPES[dtype]
+    qs = ks = [70, 133]
+    q_at = k_at = places(qs)
+    packed, kw = True, dict(causal=True)
+    if layout == "rows_of_qkv":
+        x = normal(gen, (203, 3, 4, 64), 1.5, T)
+        q, k, v = x[:, 0], x[:, 1], x[:, 2]
+    elif layout == "heads_first":
+        q, k, v = (normal(gen, (4, 203, 64), 1.5, T).transpose(0, 1) for _ in range(3))
+    elif layout == "slots":                               # a cache whose slots are taken out of order, rows to spare in each
+        q = normal(gen, (203, 4, 64), 1.5, T)
+        k, v = (normal(gen, (450, 2, 64), 1.5, T) for _ in range(2))
+        k_at, ks, packed = [300, 0], [133, 140], False
+    else:
+        q, k = (normal(gen, (203, 4, 64), 1.5, T) for _ in range(2))
+        v = normal(gen, (203, 1, 64), 1.5, T).expand(203, 4, 64)
+        k_at = places(ks)
+    out = torch.full((4, 203, 64), 7.0, dtype=T, device="cuda").transpose(0, 1) if layout == "heads_first" else None
+    check_attention(q, k, v, q_at, ks, k_at, packed=packed, dtype=dtype, **kw) if out is None else None
+    if out is not None:
+        got, _ = run_attention(q, k, v, q_at, ks, k_at, packed=True, dtype=dtype, out=out, **kw)
+        ref, _ = run_attention(q.contiguous(), k.contiguous(), v.contiguous(), q_at, ks, k_at, packed=True, dtype=dtype, **kw)
+        assert torch.equal(got, ref)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("form", ["causal_tail", "prefix", "token", "tokens_uneven", "long"])
+@pytest.mark.parametrize("poison", [math.nan, math.inf, -math.inf])
+def test_attention_passes_hidden_keys_by(form, dtype, poison):
+    """Keys that no row may see hold NaN or infinities: in front of, between and behind the sequences, and behind the last place."""
+    q, k, v, q_at, ks, k_at, kw = attention_case(form, 4, 2, 64, dtype)
+    gap = 3
+    k_at = [gap + a + gap * s for s, a in enumerate(k_at[:-1])]
+    kk, vv = (torch.full((k.shape[0] + gap * (len(ks) + 2), 2, 64), poison, dtype=k.dtype, device="cuda") for _ in range(2))
+    at = 0
+    for a, n in zip(k_at, ks):
+        kk[a:a + n], vv[a:a + n] = k[at:at + n], v[at:at + n]
+        at += n
+    check_attention(q, kk, vv, q_at, ks, k_at, packed=False, dtype=dtype, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("where", ["k", "v"])
+def test_attention_keeps_a_bad_key_to_the_rows_that_see_it(dtype, bad, where):
+    """Key 90 of 130 is bad: rows in front of it are as if it were not there, rows from it on are NaN (or infinite: its value weighs)."""
+    gen = torch.Generator().manual_seed(3)
+    q, k, v = (normal(gen, (130, 2, 64), 1.0, DTYPES[dtype]) for _ in range(3))
+    clean, clean_l = run_attention(q, k, v, [0, 130], [130], [0, 130], packed=True, dtype=dtype, causal=True)
+    (k if where == "k" else v)[90] = bad
+    got, lse = run_attention(q, k, v, [0, 130], [130], [0, 130], packed=True, dtype=dtype, causal=True)
+    ref, ref_l, mag, tol_p, tol_l = attention_f64(q, k, v, [0, 130], [130], [0, 130], causal=True)
+    half = HALF_BF16 if dtype == "bf16" else U
+    held(got[:90], ref[:90], (tol_p.unsqueeze(2)[:90] + half) * (mag[:90] + 1.0) * 8.0 + half * ref[:90].abs())
+    held(got[:90], clean[:90], 2.0 * half * 8.0)
+    bad_rows = ~torch.isfinite(ref[90:])
+    if where == "v":
+        assert bool(bad_rows.all()) and bool((~torch.isfinite(got[90:])).all())
+    else:
+        assert bool(got[90:].isnan()[ref[90:].isnan()].all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.0, 1.0, -0.5])
+def test_attention_with_steep_and_flat_scores(scale, dtype):
+    """Scores up to some hundreds: a row is all but one key's value; scale 0: the mean of the values."""
+    gen = torch.Generator().manual_seed(11)
+    q, k, v = (normal(gen, (300, 2, 64), 4.0, DTYPES[dtype]) for _ in range(3))
+    check_attention(q, k, v, [0, 300], [300], [0, 300], dtype=dtype, scale=scale)
+    check_attention(q, k, v, [0, 300], [300], [0, 300], dtype=dtype, scale=scale, cap=50.0)
+    # one query against many keys, the largest score last
+    k[299] = 3.0 * q[0] * (1.0 if scale >= 0 else -1.0)
+    check_attention(q[:1], k, v, [0, 1], [300], [0, 300], dtype=dtype, scale=scale)
+
+
+def test_attention_cuts_offsets_that_are_wrong():
+    """Offsets past the rows, decreasing or negative ones, and lengths beyond the bounds never leave the tensors."""
+    gen = torch.Generator().manual_seed(2)
+    q, k, v = (normal(gen, (60, 2, 64), 1.0, torch.bfloat16) for _ in range(3))
+    for q_at, k_at, ks in (([0, 1 << 30], [0, 1 << 30], None), ([-9, 60], [-5, 80], None), ([50, 10], [30, 20], None), ([0, 60], [40, 0], [1 << 30]), ([0, 60], [70, 0], [5]),
+                           ([0, 60], [0, 0], [-3]), ([2 ** 31 - 1, -2 ** 31], [-2 ** 31, 2 ** 31 - 1], None)):
+        out, lse = torch.zeros_like(q), torch.zeros((60, 2), device="cuda")
+        need = vpe.attention_workspace_bytes(q, k, sequences=1, max_q=60, max_k=60)
+        vpe.attention(q, k, v, out, q_offsets=i32(q_at), k_offsets=i32(k_at), k_lengths=i32(ks) if ks else None, max_q=60, max_k=60, lse=lse, causal=True,
+                      workspace=torch.empty(need, dtype=torch.uint8, device="cuda") if need else None)
+        torch.cuda.synchronize()
+        assert bool(torch.isfinite(out).all())
+    # bounds below the lengths: the queries and keys beyond them are left out
+    out, lse = run_attention(q, k, v, [0, 60], [60], [0, 60], packed=True, dtype="bf16", max_q=40, max_k=50)
+    ref, *_ = attention_f64(q[:40], k[:50], v[:50], [0, 40], [50], [0, 50])
+    assert bool((out[40:] == 7.0).all()) and float((out[:40].double() - ref).abs().max()) < 0.05
+
+
+@pytest.mark.parametrize("qs, ks, kw", [([300, 20], [300, 50], dict(causal=True, cap=20.0)), ([1, 1], [3000, 700], dict(causal=True))])
+def test_attention_in_a_graph_follows_its_arrays(qs, ks, kw):
+    """Captured once, replayed with other lengths and values, eager work of the program between the replays."""
+    gen = torch.Generator().manual_seed(8)
+    q_at, k_at = places(qs), places(ks)
+    q, k, v = normal(gen, (q_at[-1], 8, 64), 1.5, torch.bfloat16), normal(gen, (k_at[-1], 2, 64), 1.5, torch.bfloat16), normal(gen, (k_at[-1], 2, 64), 1.5, torch.bfloat16)
+    q_off, k_off, k_len = i32(q_at), i32(k_at), i32(ks)
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+    need = vpe.attention_workspace_bytes(q, k, sequences=2, max_q=max(qs), max_k=max(ks))
+    ws = torch.empty(max(need, 1), dtype=torch.uint8, device="cuda")
+
+    def call():
+        vpe.attention(q, k, v, out, q_offsets=q_off, k_offsets=k_off, k_lengths=k_len, max_q=max(qs), max_k=max(ks), lse=lse, workspace=ws,
+                      stream=torch.cuda.current_stream(), **kw)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for n, lens in enumerate(([ks[0], ks[1]], [ks[0] - 3, 1], [max(qs), ks[1]], [ks[0], 0])):
+        k_len.copy_(i32(lens))
+        q.copy_(normal(gen, q.shape, 1.0 + 0.2 * n, torch.bfloat16))
+        graph.replay()
+        torch.cuda.synchronize()
+        got, got_l = out.clone(), lse.clone()
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(got, out) and torch.equal(got_l, lse)
+        ref, *_ = attention_f64(q, k, v, q_at, lens, k_at, **kw)
+        assert float((got.double() - ref).abs().max()) < 0.08
+
+
+def test_attention_is_the_same_every_time_and_beside_another():
+    """Two calls on two streams with a workspace each, ten times: bit for bit what a call alone gives."""
+    cases = [attention_case(f, 8, 2, 64, "bf16", seed=n) for n, f in enumerate(("token_long", "views"))]
+    alone = [run_attention(q, k, v, q_at, ks, k_at, packed=True, dtype="bf16", **dict(kw)) for q, k, v, q_at, ks, k_at, kw in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(10):
+        got = []
+        for s, (q, k, v, q_at, ks, k_at, kw) in zip(streams, cases):
+            with torch.cuda.stream(s):
+                got.append(run_attention(q, k, v, q_at, ks, k_at, packed=True, dtype="bf16", stream=s, **dict(kw)))
+        torch.cuda.synchronize()
+        for (o, l), (o1, l1) in zip(got, alone):
+            assert torch.equal(o, o1) and torch.equal(l, l1)
+
+
+def test_attention_of_a_cache_past_32_bits():
+    """A cache of more than 2^32 bytes: the last slot's keys lie behind it."""
+    gen = torch.Generator().manual_seed(4)
+    rows, n = (1 << 32) // (8 * 128 * 2) + 5000, 3001
+    k = torch.zeros((rows, 8, 128), dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    k[-n:], v[-n:] = normal(gen, (n, 8, 128), 1.5, torch.bfloat16), normal(gen, (n, 8, 128), 1.5, torch.bfloat16)
+    q = normal(gen, (2, 16, 128), 1.5, torch.bfloat16)
+    out, lse = run_attention(q, k, v, [0, 1, 2], [17, n], [4, rows - n], packed=False, dtype="bf16", causal=True)
+    ref, ref_l, mag, tol_p, tol_l = attention_f64(q, k, v, [0, 1, 2], [17, n], [4, rows - n], causal=True)
+    held(out, ref, (tol_p.unsqueeze(2) + HALF_BF16) * mag + HALF_BF16 * ref.abs())
+    held(lse, ref_l, tol_l)
+
+
+# ------------------------------------------------------------------ block norm
+def norm_f64(x, *, branch=None, post=0, post_gain=None, post_bias=None, pre=0, pre_gain=None, pre_bias=None, layer_scale=None, residual_scale=1.0, gate=None,
+             scale=None, shift=None, request=None, eps=1e-6):
+    """(out, normed) and their tolerances without the rounding of normed."""
+    D = x.shape[1]
+    n = D / 64.0 + 64.0                                 # roundings in a row's sum: a lane's terms one by one, then a tree
+
+    def normal_(v, err, kind, g, b):
+        if kind == 0:
+            return v, err
+        mean = v.mean(1, keepdim=True) if kind == 1 else torch.zeros_like(v[:, :1])
+        sigma = ((v - mean).square().mean(1, keepdim=True) + eps).sqrt()
+        z = (v - mean) / sigma
+        # the mean is off by its sum's roundings, the deviation by the squares'; the input's own error enters all three
+        d = (walk(n) * v.abs().mean(1, keepdim=True) + err + err.mean(1, keepdim=True)) / sigma
+        tol = d + z.abs() * (walk(n) + d.square().mean(1, keepdim=True).sqrt()) + 4.0 * U * z.abs()
+        y = z
+        if g is not None:
+            y, tol = y * g.double(), tol * g.double().abs()
+        if b is not None:
+            y = y + b.double()
+        return y, tol + 2.0 * U * (y.abs() + (0.0 if b is None else b.double().abs()))
+
+    zero = torch.zeros_like(x, dtype=torch.float64)
+    rows = torch.zeros(x.shape[0], dtype=torch.long, device=x.device) if request is None else request.long()
+    table = [t for t in (gate, scale, shift) if t is not None]
+    mine = ((rows >= 0) & (rows < (table[0].shape[0] if table else 0))).view(-1, 1)
+
+    def of(t, neutral):
+        return zero + neutral if t is None else torch.where(mine, t.double()[rows.clamp(0, t.shape[0] - 1)], zero + neutral)
+
+    y, err = (zero, zero) if branch is None else normal_(branch.double(), zero, post, post_gain, post_bias)
+    if branch is not None:
+        f = (1.0 if layer_scale is None else layer_scale.double()) * of(gate, 1.0)
+        y, err = y * f, err * f.abs() + 3.0 * U * (y * f).abs()
+    out = residual_scale * x.double() + y
+    err = err + 2.0 * U * (out.abs() + (residual_scale * x.double()).abs())
+    h, err_h = normal_(out, err, pre, pre_gain, pre_bias)
+    m, a = 1.0 + of(scale, 0.0), of(shift, 0.0)
+    normed = h * m + a
+    return out, normed, err + 1e-37, err_h * m.abs() + 4.0 * U * ((h * m).abs() + a.abs()) + 1e-37
+
+
+def norm_case(rows, dim, dtype, gen, post, pre, requests=3, level=3.0):
+    kw = dict(branch=normal(gen, (rows, dim), 1.0, DTYPES[dtype]), post=post, pre=pre, layer_scale=normal(gen, (dim,), 0.1), residual_scale=0.81)
+    for w in ("post", "pre"):
+        kw[w + "_gain"], kw[w + "_bias"] = 1.0 + normal(gen, (dim,), 0.1), normal(gen, (dim,), 0.1)
+    for w in ("gate", "scale", "shift"):
+        kw[w] = normal(gen, (requests, dim), 0.5)
+    kw["request"] = torch.randint(-1, requests + 1, (rows,), generator=gen).int().cuda()          # -1 and `requests`: of none
+    return normal(gen, (rows, dim), 2.0) + level * normal(gen, (rows, 1)), kw
+
+
+def check_norm(x, dtype, out=None, normed=None, **kw):
+    out = torch.full_like(x, 7.0) if out is None else out
+    normed = torch.full(x.shape, 7.0, dtype=DTYPES[dtype], device="cuda") if normed is None else normed
+    ref, ref_n, tol, tol_n = norm_f64(x, **kw)
+    vpe.block_norm(x, out, normed=normed, **kw)
+    torch.cuda.synchronize()
+    held(out, ref, tol, "out")
+    held(normed, ref_n, tol_n + (HALF_BF16 if dtype == "bf16" else U) * ref_n.abs(), "normed")
+    return out, normed
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows, dim", [(1, 1), (3, 2), (5, 63), (2, 64), (7, 257), (1, 384), (9, 777), (130, 768), (4, 1000), (2, 1536), (3, 2047), (3, 2048), (2, 2049),
+                                       (5, 2052), (1, 4096), (2, 5001), (1, 8191), (3, 8192), (1025, 96)])
+def test_block_norm_against_its_definition(rows, dim, dtype):
+    gen = torch.Generator().manual_seed(rows * 10000 + dim)
+    for post, pre in ((1, 1), (2, 2), (0, 2), (1, 0)):
+        x, kw = norm_case(rows, dim, dtype, gen, post, pre)
+        check_norm(x, dtype, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [384, 777, 4096])
+def test_block_norm_leaves_out_what_is_not_given(dim, dtype):
+    gen = torch.Generator().manual_seed(dim)
+    x, kw = norm_case(6, dim, dtype, gen, 1, 2)
+    for gone in (("gate",), ("scale", "shift"), ("gate", "scale", "shift", "request"), ("post_gain", "post_bias"), ("pre_bias",), ("layer_scale",), ("branch",), ("request",)):
+        check_norm(x, dtype, **{k: v for k, v in kw.items() if k not in gone})
+    # neither branch nor norm: a scaled copy; without normed only the sum is written
+    out = torch.empty_like(x)
+    vpe.block_norm(x, out, residual_scale=-2.0)
+    assert torch.equal(out, -2.0 * x)
+    ref, *_ = norm_f64(x, **kw)
+    vpe.block_norm(x, out, **kw)
+    assert float((out.double() - ref).abs().max()) < 1e-4
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim, pitch, first", [(384, 400, 0), (384, 391, 0), (100, 100, 1), (96, 104, 3), (2050, 2060, 2)])
+def test_block_norm_of_strided_rows(dim, pitch, first, dtype):
+    """Rows inside wider ones, at any alignment of the type; what lies between them stays."""
+    gen = torch.Generator().manual_seed(pitch)
+    x, kw = norm_case(5, dim, dtype, gen, 1, 2)
+    wide = [torch.full((5 * pitch + 8,), 7.0, dtype=t, device="cuda") for t in (torch.float32, torch.float32, DTYPES[dtype], DTYPES[dtype])]
+    xs, outs, bs, ns = (w[first:first + 5 * pitch].view(5, pitch)[:, :dim] for w in wide)
+    xs.copy_(x)
+    bs.copy_(kw["branch"])
+    kw["branch"] = bs
+    check_norm(xs, dtype, out=outs, normed=ns, **kw)
+    for w in (wide[1], wide[3]):
+        assert int((w != 7.0).sum()) <= 5 * dim
+
+
+@pytest.mark.parametrize("dim", [768, 8192])
+def test_block_norm_in_place_and_in_a_graph(dim):
+    gen = torch.Generator().manual_seed(1)
+    x, kw = norm_case(40, dim, "bf16", gen, 2, 1)
+    want, want_n = check_norm(x, "bf16", **kw)
+    mine, normed = x.clone(), torch.empty((40, dim), dtype=torch.bfloat16, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    vpe.block_norm(mine, mine, normed=normed, stream=torch.cuda.current_stream(), **kw)
+    torch.cuda.synchronize()
+    assert torch.equal(mine, want) and torch.equal(normed, want_n)
+    with torch.cuda.graph(graph):
+        vpe.block_norm(mine, mine, normed=normed, stream=torch.cuda.current_stream(), **kw)
+    for n in range(3):
+        mine.copy_(x * (n + 1))
+        graph.replay()
+        torch.cuda.synchronize()
+        again, again_n = torch.empty_like(x), torch.empty_like(normed)
+        vpe.block_norm(x * (n + 1), again, normed=again_n, **kw)
+        torch.cuda.synchronize()
+        assert torch.equal(mine, again) and torch.equal(normed, again_n)
+
+
+def test_block_norm_of_rows_far_from_zero_and_of_bad_ones():
+    gen = torch.Generator().manual_seed(6)
+    x, kw = norm_case(8, 1536, "f32", gen, 1, 1, level=1000.0)
+    check_norm(x, "f32", **kw)
+    x[3, 5], x[5, 0] = math.nan, math.inf
+    out, normed = torch.empty_like(x), torch.empty_like(x)
+    vpe.block_norm(x, out, normed=normed, **kw)
+    bad = ~torch.isfinite(normed).all(1)
+    assert bad.tolist() == [False] * 3 + [True, False, True, False, False] and bool(normed[3].isnan().all()) and bool(normed[5].isnan().all())
+    # rows of equal values: eps decides, nothing divides by zero
+    same = torch.full((3, 640), 2.5, device="cuda")
+    vpe.block_norm(same, out[:3, :640], normed=normed[:3, :640], pre=vpe.VPE_NORM_LAYER)
+    assert bool((normed[:3, :640] == 0.0).all())
+
+
+# ------------------------------------------------------------------ adapters
+def adapters_f64(x, w, bias=None, a=None, b=None, adapter=None, scale=None):
+    """Result in 64 bits, and its tolerance for fp32 sums without the rounding of the result."""
+    X, W = x.double(), w.double()
+    y = X @ W.t().contiguous()
+    K = x.shape[1]
+    tol = walk(K) * (X.abs() @ W.abs().t().contiguous())
+    if bias is not None:
+        y = y + bias.double()
+    if a is not None:
+        for n in range(a.shape[0]):
+            rows = torch.nonzero(adapter == n).flatten()
+            if not len(rows):
+                continue
+            A, B = a[n].double().t().contiguous(), b[n].double().t().contiguous()
+            s = 1.0 if scale is None else float(scale[n])
+            t = s * (X[rows] @ A)
+            y[rows] += t @ B
+            # the low-rank values: their own sums' roundings, two bf16 terms (2^-17 of the value), the second sum
+            dt = abs(s) * walk(K) * (X[rows].abs() @ A.abs()) + (2.0 ** -17 + 4.0 * U) * t.abs()
+            tol[rows] += dt @ B.abs() + walk(a.shape[1]) * (t.abs() @ B.abs())
+    return y, tol + 4.0 * U * y.abs()
+
+
+def adapter_case(rows, k, n, rank, adapters, dtype, mode, seed=0):
+    gen, T = torch.Generator().manual_seed(seed + rows + k + n), DTYPES[dtype]
+    x, w = normal(gen, (rows, k), 1.0, T), normal(gen, (n, k), k ** -0.5, T)
+    kw = dict(bias=normal(gen, (n,), 0.2))
+    if adapters:
+        kw.update(a=normal(gen, (adapters, rank, k), k ** -0.5, T), b=normal(gen, (adapters, n, rank), 0.5, T), scale=0.5 + normal(gen, (adapters,), 0.3).abs())
+        which = {"grouped": torch.arange(rows) * adapters // max(rows, 1), "mixed": torch.randint(-1, adapters + 1, (rows,), generator=gen),
+                 "none": torch.full((rows,), -1), "last": torch.full((rows,), adapters - 1)}[mode]
+        kw["adapter"] = which.int().cuda()
+    return x, w, kw
+
+
+def check_adapters(x, w, out=None, **kw):
+    out = torch.full((x.shape[0], w.shape[0]), 7.0, dtype=x.dtype, device="cuda") if out is None else out
+    need = vpe.adapter_linear_workspace_bytes(x, w, kw.get("a"))
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda") if need else None
+    vpe.adapter_linear(x, w, out, workspace=ws, **kw)
+    ref, tol = adapters_f64(x, w, **kw)
+    torch.cuda.synchronize()
+    held(out, ref, tol + (HALF_BF16 * ref.abs() if out.dtype == torch.bfloat16 else 0.0), "out")
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows, k, n, rank, adapters, mode", [
+    (1, 64, 1, 8, 1, "last"), (1, 384, 1152, 16, 4, "grouped"), (2, 128, 7, 8, 3, "mixed"), (5, 256, 100, 24, 5, "mixed"), (16, 1024, 333, 64, 7, "mixed"),
+    (17, 64, 64, 128, 2, "grouped"), (33, 448, 257, 40, 40, "mixed"), (48, 512, 1536, 16, 32, "mixed"), (64, 192, 65, 8, 1, "none"), (130, 384, 384, 16, 3, "grouped"),
+    (257, 320, 1000, 8, 2, "grouped"), (300, 64, 4000, 120, 9, "mixed"), (1531, 384, 1152, 32, 5, "grouped"), (1400, 256, 130, 16, 64, "mixed"),
+    (700, 1536, 1536, 16, 3, "grouped"), (100, 768, 2304, 16, 0, "none")])
+def test_adapters_against_their_definition(rows, k, n, rank, adapters, mode, dtype):
+    x, w, kw = adapter_case(rows, k, n, rank, adapters, dtype, mode)
+    check_adapters(x, w, **kw)
+    kw.pop("bias")
+    kw.pop("scale", None)
+    check_adapters(x, w, out=torch.full((rows, n), 7.0, device="cuda"), **kw)
+
+
+def test_adapters_of_a_large_problem():
+    """Whole rounds of the largest tiles and rows that are left over."""
+    x, w, kw = adapter_case(10992, 512, 1536, 32, 8, "bf16", "grouped")
+    check_adapters(x, w, **kw)
+    kw["adapter"] = torch.randint(-1, 8, (10992,), generator=torch.Generator().manual_seed(1)).int().cuda()
+    check_adapters(x, w, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [3, 200])
+def test_adapters_of_strided_rows(rows, dtype):
+    """x inside wider rows, out inside wider rows at an odd pitch and place: what lies between stays."""
+    x, w, kw = adapter_case(rows, 256, 130, 16, 4, dtype, "mixed")
+    wide_x = torch.full((rows, 320), math.nan, dtype=x.dtype, device="cuda")
+    wide_x[:, 8:264] = x
+    flat = torch.full((rows * 137 + 3,), 7.0, dtype=x.dtype, device="cuda")
+    out = flat[3:].view(rows, 137)[:, :130]
+    check_adapters(wide_x[:, 8:264], w, out=out, **kw)
+    assert bool((flat[:3] == 7.0).all()) and bool((flat[3:].view(rows, 137)[:, 130:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [4, 150])
+def test_adapters_keep_bad_values_to_their_rows(rows, dtype):
+    """A row of infinities, an adapter of NaN and a weight row of NaN reach the rows and the columns that use them, and no other."""
+    x, w, kw = adapter_case(rows, 192, 140, 16, 3, dtype, "grouped")
+    kw["adapter"][1] = 2
+    clean = check_adapters(x, w, **kw)
+    kw["adapter"][:1] = 0
+    kw["a"][1], kw["b"][1] = math.nan, math.inf
+    kw["adapter"][kw["adapter"] == 1] = -1
+    x[2] = math.inf
+    w[70] = math.nan
+    ws = torch.empty(vpe.adapter_linear_workspace_bytes(x, w, kw["a"]), dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(clean)
+    vpe.adapter_linear(x, w, out, workspace=ws, **kw)
+    ref, tol = adapters_f64(x, w, **kw)
+    rows_ok = torch.ones(rows, dtype=torch.bool, device="cuda")
+    rows_ok[2] = False
+    cols_ok = torch.ones(140, dtype=torch.bool, device="cuda")
+    cols_ok[70] = False
+    got = out[rows_ok][:, cols_ok]
+    assert bool(torch.isfinite(got).all()) and bool((~torch.isfinite(out[2])).all()) and bool(out[:, 70].isnan().all())
+    held(got, ref[rows_ok][:, cols_ok], (tol + (HALF_BF16 if dtype == "bf16" else 0.0) * ref.abs())[rows_ok][:, cols_ok])
+
+
+@pytest.mark.parametrize("rows", [6, 400])
+def test_adapters_in_a_graph_follow_their_rows(rows):
+    x, w, kw = adapter_case(rows, 384, 512, 16, 5, "bf16", "mixed")
+    ws = torch.empty(vpe.adapter_linear_workspace_bytes(x, w, kw["a"]), dtype=torch.uint8, device="cuda")
+    out = torch.empty((rows, 512), dtype=torch.bfloat16, device="cuda")
+
+    def call():
+        vpe.adapter_linear(x, w, out, workspace=ws, stream=torch.cuda.current_stream(), **kw)
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    gen = torch.Generator().manual_seed(1)
+    for _ in range(4):
+        kw["adapter"].copy_(torch.randint(-1, 5, (rows,), generator=gen).int())
+        x.copy_(normal(gen, x.shape, 1.0, torch.bfloat16))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(got, out)
+        ref, tol = adapters_f64(x, w, **kw)
+        held(got, ref, tol + HALF_BF16 * ref.abs())
+
+
+# ------------------------------------------------------------------ together
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_block_for_packed_requests(dtype):
+    """norm, adapted QKV, attention, adapted out-projection, norm: views of three requests through one block, on a stream of its own, against
+    64 bits.  Every stage's rounding reaches the result: bf16 rounds normed, qkv, the probabilities, the attention's result and the
+    projection (five times 2^-8 of values whose size the weights keep near one)."""
+    D, H, T = 384, 6, DTYPES[dtype]
+    gen = torch.Generator().manual_seed(21)
+    lens = [257, 64, 130]
+    at, rows = places(lens), sum(lens)
+    request = torch.cat([torch.full((n,), s) for s, n in enumerate(lens)]).int().cuda()
+    x = normal(gen, (rows, D), 1.5)
+    wq, wo = normal(gen, (3 * D, D), D ** -0.5, T), normal(gen, (D, D), D ** -0.5, T)
+    aq, bq = normal(gen, (3, 16, D), D ** -0.5, T), normal(gen, (3, 3 * D, 16), 0.1, T)
+    ao, bo = normal(gen, (3, 16, D), D ** -0.5, T), normal(gen, (3, D, 16), 0.1, T)
+    gate, scale, shift = (normal(gen, (3, D), 0.2) for _ in range(3))
+    g = 1.0 + normal(gen, (D,), 0.1)
+    slopes = torch.exp2(-torch.arange(1, H + 1, dtype=torch.float32)).cuda()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        h, qkv = torch.empty((rows, D), dtype=T, device="cuda"), torch.empty((rows, 3 * D), dtype=T, device="cuda")
+        o, y = torch.empty((rows, D), dtype=T, device="cuda"), torch.empty((rows, D), dtype=T, device="cuda")
+        x1, x2, h2 = torch.empty_like(x), torch.empty_like(x), torch.empty_like(h)
+        off = i32(at)
+        view = qkv.view(rows, 3, H, 64)
+        ws = torch.empty(max(vpe.adapter_linear_workspace_bytes(h, wq, aq), vpe.attention_workspace_bytes(view[:, 0], view[:, 1], sequences=3, max_q=257, max_k=257), 1),
+                         dtype=torch.uint8, device="cuda")
+        vpe.block_norm(x, x1, normed=h, pre=vpe.VPE_NORM_LAYER, pre_gain=g, scale=scale, shift=shift, request=request, stream=s)
+        vpe.adapter_linear(h, wq, qkv, a=aq, b=bq, adapter=request, workspace=ws, stream=s)
+        vpe.attention(view[:, 0], view[:, 1], view[:, 2], o.view(rows, H, 64), q_offsets=off, k_offsets=off, max_q=257, max_k=257, cap=20.0, slopes=slopes,
+                      workspace=ws, stream=s)
+        vpe.adapter_linear(o, wo, y, a=ao, b=bo, adapter=request, workspace=ws, stream=s)
+        vpe.block_norm(x1, x2, branch=y, normed=h2, post=vpe.VPE_NORM_RMS, pre=vpe.VPE_NORM_LAYER, gate=gate, scale=scale, shift=shift, request=request, stream=s)
+    s.synchronize()
+    _, rh, _, _ = norm_f64(x, pre=1, pre_gain=g, scale=scale, shift=shift, request=request)
+    rq, _ = adapters_f64(rh, wq, a=aq, b=bq, adapter=request)
+    rv = rq.view(rows, 3, H, 64)
+    ro, *_ = attention_f64(rv[:, 0], rv[:, 1], rv[:, 2], at, lens, at, cap=20.0, slopes=slopes)
+    ry, _ = adapters_f64(ro.view(rows, D), wo, a=ao, b=bo, adapter=request)
+    r2, rn, _, _ = norm_f64(x, branch=ry, post=2, pre=1, gate=gate, scale=scale, shift=shift, request=request)
+    rel = lambda got, ref: float((got.double() - ref).norm() / ref.norm())  # noqa: E731
+    # five roundings of bf16 add up to at most 5 x 2^-8 in the norm; fp32: sums of up to 384 terms, four stages
+    bound = 5.0 * HALF_BF16 if dtype == "bf16" else 8.0 * walk(D)
+    assert torch.equal(x1, x)
+    assert rel(y, ry) < bound and rel(x2, r2) < bound and rel(h2, rn) < bound
