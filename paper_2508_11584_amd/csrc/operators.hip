@@ -30,6 +30,7 @@ int check_sizes(const vpe_attention_args* a) {
     if (a->dtype != VPE_F32 && a->dtype != VPE_BF16) REFUSE("unknown dtype");
     if (a->head_dim != 64 && a->head_dim != 128) REFUSE("head_dim is %d: 64 or 128 required", a->head_dim);
     if (a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads || a->heads > 4096) REFUSE("heads must be a multiple of kv_heads, at most 4096");
+    if (a->sequences > (1 << 24)) REFUSE("more than 2^24 sequences");
     if (a->sequences < 0 || a->max_q < 0 || a->max_k < 0 || a->q_rows < 0 || a->k_rows < 0) REFUSE("sizes must not be negative");
     // (row places are 32-bit sums of two lengths; a workspace row count stays below 2^31)
     if (a->q_rows > (1 << 30) || a->k_rows > (1 << 30) || a->max_q > (1 << 30) || a->max_k > (1 << 30)) REFUSE("more than 2^30 rows");
@@ -78,6 +79,7 @@ int vpe_attention(const vpe_attention_args* args, void* stream) {
     const int per16 = a.dtype == VPE_BF16 ? 8 : 4;
     for (int64_t v : {a.q_row, a.q_head, a.k_row, a.k_head, a.v_row, a.v_head, a.out_row, a.out_head})
         if (v % per16) REFUSE("strides must be multiples of 16 bytes");
+    if (a.k_row > (1 << 23) || a.v_row > (1 << 23)) REFUSE("row strides of k and v above 2^23 elements");      // (a tile's offsets are 32-bit)
     if (nothing_to_do(a)) return VPE_OK;
     if (!a.q || !a.out || !a.q_offsets || !a.k_offsets) REFUSE("null pointer");
     if (a.k_rows > 0 && a.max_k > 0 && (!a.k || !a.v)) REFUSE("k or v is null");

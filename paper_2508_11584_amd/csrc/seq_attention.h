@@ -3,7 +3,10 @@
 //   s_ij = scale q_i.k_j;  cap > 0: s = cap tanh(s / cap);  s -= slope_h dist(i, j)
 //   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(s_ij - m_i) over the keys j that row i sees,  lse_i = m_i + log sum_j p_ij
 #pragma once
+#include "attention.h"
 #include "common.h"
+#include "gemm_dma.h"
+#include "split3.h"
 #include "vpe.h"
 
 namespace vpe {
@@ -28,10 +31,43 @@ __device__ __forceinline__ Seq sequence(const vpe_attention_args& p, int s) {
     return r;
 }
 
-// Row i of sequence `sq`, head h, by one wave in plain fp32: 64 keys at a time, a lane has a key's score and then one or two
-// columns of the result.  Keys that the row does not see are never read: nothing they hold can reach the result.
+// What a call's launches share beyond its arguments.
+struct SeqAttnGrid {
+    int blocks, packed, splits, per_split;
+    float *part_o, *part_ml;     // splits > 1: [split][q_rows][heads][D] sums against the part's reference, [split][q_rows][heads][2] (reference, sum)
+};
+
+// Keys that the row at `place` sees: 0 .. limit - 1.  (Causal rows see what is before them and the prefix: one range.)
+__device__ __forceinline__ int key_limit(const vpe_attention_args& p, const Seq& sq, int place) {
+    if (!p.causal) return sq.nk;
+    const int n = place + 1 > sq.prefix ? place + 1 : sq.prefix;
+    return n < 0 ? 0 : n < sq.nk ? n : sq.nk;
+}
+
+// Leaves columns c .. c + N - 1 of a row: the result, or with several parts of the keys the part's sum.
+template <int N, typename T>
+__device__ __forceinline__ void store_columns(T* dst, const float* v) {
+    T e[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) e[i] = from_f32<T>(v[i]);
+    typedef uint32_t Raw __attribute__((ext_vector_type(N * sizeof(T) / 4)));
+    Raw raw;
+    __builtin_memcpy(&raw, e, sizeof raw);
+    *reinterpret_cast<Raw*>(dst) = raw;
+}
+__device__ __forceinline__ int64_t part_row(const vpe_attention_args& p, int64_t row, int h, int split) { return ((int64_t)split * p.q_rows + row) * p.heads + h; }
+template <typename T>
+__device__ __forceinline__ void store_stats(const vpe_attention_args& p, const SeqAttnGrid& g, int64_t row, int h, int split, float m, float l) {
+    if (g.splits > 1) *reinterpret_cast<f32x2*>(g.part_ml + 2 * part_row(p, row, h, split)) = f32x2{m, l};
+    else if (p.lse) p.lse[row * p.heads + h] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
+}
+
+// Row i of sequence `sq`, head h, over the keys j_begin .. j_end - 1, by one wave in plain fp32: 64 keys at a time, a lane has a key's
+// score and then one or two columns of the result.  Keys that the row does not see are never read, so nothing they hold can reach the
+// result, and infinite or NaN scores and values come out as the definition has them: the tiled kernel hands the rows over here whose sums
+// are not finite.  (A call of nothing but such rows is 10-40 times as long as one of none.)
 template <typename T, int D>
-__device__ __forceinline__ void attention_row(const vpe_attention_args& p, const Seq& sq, int i, int h, int lane) {
+__device__ __forceinline__ void attention_row(const vpe_attention_args& p, const SeqAttnGrid& g, const Seq& sq, int i, int h, int j_begin, int j_end, int split, int lane) {
     constexpr int CE = Elem<T>::CE, ND = D / 64;
     const int kh = h / (p.heads / p.kv_heads), place = i + sq.nk - sq.nq;
     const int64_t row = sq.q0 + i;
@@ -44,16 +80,14 @@ __device__ __forceinline__ void attention_row(const vpe_attention_args& p, const
     float qv[ND], acc[ND], m = -INFINITY, l = 0.0f;
 #pragma unroll
     for (int n = 0; n < ND; ++n) { qv[n] = to_f32(q[64 * n + lane]); acc[n] = 0.0f; }
-    for (int j0 = 0; j0 < sq.nk; j0 += 64) {
-        const int j = j0 + lane;
-        const bool seen = j < sq.nk && (!p.causal || j <= place || j < sq.prefix);
-        const uint64_t any = __ballot(seen);
-        if (!any) continue;
+    const int limit = key_limit(p, sq, place), end = limit < j_end ? limit : j_end;
+    for (int j0 = j_begin; j0 < end; j0 += 64) {
+        const int j = j0 + lane < end ? j0 + lane : end - 1, n_here = end - j0 < 64 ? end - j0 : 64;
         float s = 0.0f;
-        const T* kr = k + (int64_t)(seen ? j : j0 + __builtin_ctzll(any)) * p.k_row;
+        const T* kr = k + (int64_t)j * p.k_row;
 #pragma unroll
         for (int n = 0; n < ND; ++n)
-#pragma unroll 2
+#pragma unroll 1
             for (int d = 0; d < 64; d += CE) {
                 const u32x4 raw = *reinterpret_cast<const u32x4*>(kr + 64 * n + d);
                 T e[CE];
@@ -64,13 +98,13 @@ __device__ __forceinline__ void attention_row(const vpe_attention_args& p, const
         s *= p.scale;
         if (p.cap > 0.0f) s = p.cap * tanhf(s / p.cap);
         if (p.q_coords) {
-            const f32x2 to = *reinterpret_cast<const f32x2*>(p.k_coords + 2 * (int64_t)(sq.k0 + (seen ? j : j0)));
+            const f32x2 to = *reinterpret_cast<const f32x2*>(p.k_coords + 2 * (int64_t)(sq.k0 + j));
             const float dy = at[0] - to[0], dx = at[1] - to[1];
             s -= slope * sqrtf(dy * dy + dx * dx);
         } else if (p.slopes) {
             s -= slope * fabsf((float)(place - j));
         }
-        s = seen ? s * LOG2E : -INFINITY;
+        s = lane < n_here ? s * LOG2E : -INFINITY;
         float mx = s;
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
@@ -82,18 +116,578 @@ __device__ __forceinline__ void attention_row(const vpe_attention_args& p, const
         m = top;
 #pragma unroll
         for (int n = 0; n < ND; ++n) acc[n] *= alpha;
-        for (uint64_t left = any; left; left &= left - 1) {
-            const int jj = __builtin_ctzll(left);
+        for (int jj = 0; jj < n_here; ++jj) {
             const float pj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e), jj));
             const T* vr = v + (int64_t)(j0 + jj) * p.v_row;
 #pragma unroll
             for (int n = 0; n < ND; ++n) acc[n] = fmaf(pj, to_f32(vr[64 * n + lane]), acc[n]);
         }
     }
-    T* out = reinterpret_cast<T*>(p.out) + row * p.out_row + h * p.out_head;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float inv = g.splits > 1 ? 1.0f : 1.0f / l;
 #pragma unroll
-    for (int n = 0; n < ND; ++n) out[64 * n + lane] = from_f32<T>(l == 0.0f ? 0.0f : acc[n] * inv);
+    for (int n = 0; n < ND; ++n) {
+        const float r = l == 0.0f ? 0.0f : acc[n] * inv;
+        if (g.splits > 1) g.part_o[part_row(p, row, h, split) * D + 64 * n + lane] = r;
+        else reinterpret_cast<T*>(p.out)[row * p.out_row + h * p.out_head + 64 * n + lane] = from_f32<T>(r);
+    }
+    if (lane == 0) store_stats<T>(p, g, row, h, split, m, l);
+}
+
+// --- matrix pieces: 32 x 32 blocks, 16 k elements a step; a lane (li = lane % 32, h = lane / 32) gives row li's eight elements
+// 8 h .. 8 h + 7 of a step, and holds of a result column li rows 8 (v / 4) + 4 h + v % 4, v = 0 .. 15.
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char LdsByte;
+
+template <typename T, int D> struct SeqMma;
+
+template <int D> struct SeqMma<bf16, D> {
+    typedef bf16x8 Frag;
+    static constexpr int ROWB = 2 * D;                // bytes of a tile row; 16-byte chunks are exchanged by the row:
+    // 16 consecutive rows reading one chunk of the keys fall on different banks;
+    static __device__ __forceinline__ int k_swz(int r) { return D == 64 ? (r >> 1) & 7 : r & 15; }
+    // four consecutive rows reading the same 64 bytes of the values do (the transposing read below)
+    static __device__ __forceinline__ int v_swz(int r) { return D == 64 ? ((r >> 1) & 1) << 2 : (r & 3) << 2; }
+    static __device__ __forceinline__ Frag load(const bf16* src) { return *reinterpret_cast<const bf16x8*>(src); }
+    static __device__ __forceinline__ Frag k_frag(const char* tile, int row, int ks, int g) {
+        return *reinterpret_cast<const bf16x8*>(tile + row * ROWB + (((2 * ks + g) ^ k_swz(row)) << 4));
+    }
+    // Values as the second product's first operand: of columns 32 d + li the keys 16 st + 4 g .. + 3 and 16 st + 8 + 4 g .. + 3 (where a score
+    // block's column has its probabilities).  ds_read_b64_tr_b16 gives lane i of 16 column i of the four rows whose 32 bytes those lanes
+    // address.  Eight reads and the wait for them are one block of assembly: for the builtin the compiler waits for all loads into the LDS
+    // that are under way, the next tile's.  A block holds STEPS steps of 16 keys, from step `st` on.
+    static constexpr int STEPS = D == 64 ? 2 : 1;
+    struct Values { uint32_t at[D / 32]; };              // LDS address of the lane's read of tile row 0, by column block
+    static __device__ __forceinline__ Values values(const char* tile, int lane) {
+        const int t = lane & 15, row = 4 * (lane >> 5) + (t >> 2);
+        Values v;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) {
+            const int chunk = 4 * d + 2 * ((lane >> 4) & 1) + ((t >> 1) & 1);
+            v.at[d] = (uint32_t)(uintptr_t)(LdsByte*)tile + row * ROWB + ((chunk ^ v_swz(row)) << 4) + (t & 1) * 8;      // (rows 8 apart have the same exchange)
+        }
+        return v;
+    }
+    template <int ST>
+    static __device__ __forceinline__ void v_frags(const Values& a, Frag (&f)[STEPS][D / 32]) {
+        constexpr int Z = 16 * ST * ROWB;
+        u32x2 r[8];
+        if constexpr (D == 64) {
+            asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%c10\n\tds_read_b64_tr_b16 %1, %8 offset:%c11\n\t"
+                         "ds_read_b64_tr_b16 %2, %9 offset:%c10\n\tds_read_b64_tr_b16 %3, %9 offset:%c11\n\t"
+                         "ds_read_b64_tr_b16 %4, %8 offset:%c12\n\tds_read_b64_tr_b16 %5, %8 offset:%c13\n\t"
+                         "ds_read_b64_tr_b16 %6, %9 offset:%c12\n\tds_read_b64_tr_b16 %7, %9 offset:%c13\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+                         : "v"(a.at[0]), "v"(a.at[1]), "n"(Z), "n"(Z + 8 * ROWB), "n"(Z + 16 * ROWB), "n"(Z + 24 * ROWB)
+                         : "memory");
+        } else {
+            asm volatile("ds_read_b64_tr_b16 %0, %8 offset:%c12\n\tds_read_b64_tr_b16 %1, %8 offset:%c13\n\t"
+                         "ds_read_b64_tr_b16 %2, %9 offset:%c12\n\tds_read_b64_tr_b16 %3, %9 offset:%c13\n\t"
+                         "ds_read_b64_tr_b16 %4, %10 offset:%c12\n\tds_read_b64_tr_b16 %5, %10 offset:%c13\n\t"
+                         "ds_read_b64_tr_b16 %6, %11 offset:%c12\n\tds_read_b64_tr_b16 %7, %11 offset:%c13\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+                         : "v"(a.at[0]), "v"(a.at[1]), "v"(a.at[2]), "v"(a.at[3]), "n"(Z), "n"(Z + 8 * ROWB)
+                         : "memory");
+        }
+#pragma unroll
+        for (int n = 0; n < 4; ++n) f[n / (D / 32)][n % (D / 32)] = __builtin_bit_cast(bf16x8, u32x4{r[2 * n][0], r[2 * n][1], r[2 * n + 1][0], r[2 * n + 1][1]});
+    }
+    static __device__ __forceinline__ Frag probs(const float* e) {
+        bf16x8 b;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = (bf16)e[i];
+        return b;
+    }
+    static __device__ __forceinline__ f32x16 mma(const Frag& a, const Frag& b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+
+// fp32: three bf16 terms per operand (split3.h), six products.
+template <int D> struct SeqMma<float, D> {
+    typedef Split3 Frag;
+    static constexpr int ROWB = 4 * D;
+    // (the values are read element by element, two keys four rows apart at once: they fall on different halves of the banks)
+    static __device__ __forceinline__ int k_swz(int r) { return (r & 3) | (r & 4) << 1 | (r & 8) >> 1; }
+    static __device__ __forceinline__ int v_swz(int r) { return k_swz(r); }
+    static __device__ __forceinline__ Frag load(const float* src) { return split3(*reinterpret_cast<const f32x4*>(src), *reinterpret_cast<const f32x4*>(src + 4)); }
+    static __device__ __forceinline__ Frag k_frag(const char* tile, int row, int ks, int g) {
+        const char* at = tile + row * ROWB;
+        const int c = 4 * ks + 2 * g, sw = k_swz(row);
+        return split3(*reinterpret_cast<const f32x4*>(at + ((c ^ sw) << 4)), *reinterpret_cast<const f32x4*>(at + (((c + 1) ^ sw) << 4)));
+    }
+    static constexpr int STEPS = 1;
+    struct Values { const char* tile; int lane; };
+    static __device__ __forceinline__ Values values(const char* tile, int lane) { return {tile, lane}; }
+    template <int ST>
+    static __device__ __forceinline__ void v_frags(const Values& a, Frag (&f)[1][D / 32]) {
+        const int li = a.lane & 31, g = a.lane >> 5;
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) {
+            f32x4 e[2];
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = 16 * ST + 8 * n + 4 * g + i;
+                    e[n][i] = *reinterpret_cast<const float*>(a.tile + row * ROWB + (((8 * d + (li >> 2)) ^ v_swz(row)) << 4) + (li & 3) * 4);
+                }
+            f[0][d] = split3(e[0], e[1]);
+        }
+    }
+    static __device__ __forceinline__ Frag probs(const float* e) { return split3(f32x4{e[0], e[1], e[2], e[3]}, f32x4{e[4], e[5], e[6], e[7]}); }
+    static __device__ __forceinline__ f32x16 mma(const Frag& a, const Frag& b, f32x16 c) {
+#pragma unroll
+        for (int t = 0; t < 6; ++t) c = split_mma(t, a, b, c);
+        return c;
+    }
+};
+
+// What a score goes through between the two products: nothing but its factor (PLAIN), a cap and distances in a line (LINE), a cap and
+// distances between coordinates (GRID).
+enum { SCORES_PLAIN = 0, SCORES_LINE = 1, SCORES_GRID = 2 };
+
+template <typename T, int D, int KT, int KW, int MODE>
+constexpr int seq_stage_bytes() { return KW * (2 * KT * SeqMma<T, D>::ROWB + (MODE == SCORES_GRID ? KT * 8 : 0)); }
+template <typename T, int D, int KT, int QW, int KW, int MODE>
+constexpr int seq_lds_bytes() {
+    const int stages = 2 * seq_stage_bytes<T, D, KT, KW, MODE>(), merge = KW > 1 ? KW * 32 * (D + 2) * 4 + 64 : 0;
+    return stages > merge ? stages : merge;
+}
+
+// A workgroup takes 32 QW consecutive rows of a sequence and key head and the keys of one part; a row is a query and one of the G =
+// heads / kv_heads query heads that read the key head (row r: query r / G, head r % G), so those share every tile.  QW waves of 32 rows
+// share the tiles (KW = 1), or KW waves have all 32 rows and every KW-th tile (QW = 1) and their results meet in LDS, in a fixed order.
+// A wave computes scores transposed, S^T = K Q^T: a lane holds half of one row's scores, reductions over the keys stay in the lane but for one
+// exchange, and the probabilities are the second product's operand, O^T = V^T P^T, as they lie.
+template <typename T, int D, int KT, int QW, int KW, int MODE, int OCC>
+__global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const vpe_attention_args p, const SeqAttnGrid grid) {
+    static_assert(QW == 1 || KW == 1, "tiles are shared by all waves or by none");
+    using M = SeqMma<T, D>;
+    typedef typename M::Frag Frag;
+    constexpr int NW = QW * KW, ROWB = M::ROWB, TILE = KT * ROWB, OWN = 2 * TILE + (MODE == SCORES_GRID ? KT * 8 : 0), STAGE = KW * OWN;
+    constexpr int NB = KT / 32, DB = D / 32, KS = D / 16, CE = Elem<T>::CE;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int qw = QW > 1 ? wave : 0, kw = KW > 1 ? wave : 0, g = lane >> 5, li = lane & 31;
+    const int G = p.heads / p.kv_heads;
+
+    // --- which rows: consecutive workgroups of an XCD have the same keys; the longest row blocks of causal calls come first
+    int lin = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int split = lin % grid.splits;
+    lin /= grid.splits;
+    int blk = lin % grid.blocks, s = 0, kh;
+    if (grid.packed) {
+        kh = lin / grid.blocks;
+        // the sequence that has row block `blk` of all: 64 sequences at a time, a lane counts one's blocks
+        int before = 0;
+        for (int s0 = 0;; s0 += 64) {
+            if (s0 >= p.sequences) return;
+            int n = 0, q0;
+            if (s0 + lane < p.sequences) n = (int)(((int64_t)seq_rows(p, s0 + lane, q0) * G + 32 * QW - 1) / (32 * QW));
+            int sum = n;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int t = __shfl_up(sum, o);
+                if (lane >= o) sum += t;
+            }
+            const uint64_t past = __ballot(before + sum > blk);
+            if (past) {
+                const int at = __builtin_ctzll(past);
+                s = s0 + at;
+                blk -= before + __shfl(sum - n, at);
+                break;
+            }
+            before += __shfl(sum, 63);
+        }
+        s = __builtin_amdgcn_readfirstlane(s);
+        blk = __builtin_amdgcn_readfirstlane(blk);
+        if (blk < 0) return;                             // (offsets that make no sense: their counts may have wrapped)
+    } else {
+        const int sk = lin / grid.blocks;
+        kh = sk % p.kv_heads;
+        s = sk / p.kv_heads;
+    }
+    const Seq sq = sequence(p, s);
+    const int64_t rows = (int64_t)sq.nq * G;
+    if (p.causal) {                                      // (blocks that the sequence does not have stay where they are)
+        const int mine = (int)((rows + 32 * QW - 1) / (32 * QW));
+        if (blk < mine) blk = mine - 1 - blk;
+    }
+    const int64_t r0 = (int64_t)blk * 32 * QW;
+    if (r0 >= rows) return;
+    const int64_t r = r0 + qw * 32 + li;
+    const bool real = r < rows;
+    const int i = (int)((real ? r : rows - 1) / G), h = kh * G + (int)((real ? r : rows - 1) - (int64_t)i * G);
+    const int place = i + sq.nk - sq.nq, limit = real ? key_limit(p, sq, place) : 0;
+    const int64_t row = sq.q0 + i;
+
+    // keys of this part that any row of the workgroup sees: the last row's (limits do not fall)
+    const int64_t r_last = r0 + 32 * QW < rows ? r0 + 32 * QW - 1 : rows - 1;
+    const int wg_limit = key_limit(p, sq, (int)(r_last / G) + sq.nk - sq.nq);
+    const int j_begin = split * grid.per_split, j_stop = j_begin + grid.per_split;           // (plan: fits 32 bits)
+    const int j_end = wg_limit < j_stop ? wg_limit : j_stop;
+    const int tiles = j_end > j_begin ? (j_end - j_begin + KT - 1) / KT : 0;
+    // the wave's own range of limits: tiles below the smallest need no mask, tiles past the largest no work
+    int lim_min = real ? limit : 0x7fffffff, lim_max = limit;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int a = __shfl_xor(lim_min, o), b = __shfl_xor(lim_max, o);
+        lim_min = a < lim_min ? a : lim_min;
+        lim_max = b > lim_max ? b : lim_max;
+    }
+    lim_min = __builtin_amdgcn_readfirstlane(lim_min);
+    lim_max = __builtin_amdgcn_readfirstlane(lim_max);
+
+    // --- loader: an instruction of a wave fills 1 KB, lane l the 16-byte chunk l of it; the lane fetches the chunk that belongs there
+    constexpr int CPR = ROWB / 16, RPI = 64 / CPR, LW = KW > 1 ? 1 : QW, NI = TILE / 1024 / LW;
+    static_assert(TILE % (1024 * LW) == 0, "whole instructions");
+    const int lw = KW > 1 ? 0 : wave;
+    const T* kbase = reinterpret_cast<const T*>(p.k) + (int64_t)sq.k0 * p.k_row + kh * p.k_head;
+    const T* vbase = reinterpret_cast<const T*>(p.v) + (int64_t)sq.k0 * p.v_row + kh * p.v_head;
+    auto dma = [&](char* stage, int t) {                 // keys j0 .. j0 + KT - 1, those from j_end on as the last of them
+        const int j0 = j_begin + t * KT, last = j_end - 1 - j0;
+        char* own = stage + kw * OWN;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            const char* base = reinterpret_cast<const char*>((which ? vbase : kbase) + (int64_t)j0 * (which ? p.v_row : p.k_row));
+            const uint32_t pitch = (uint32_t)(which ? p.v_row : p.k_row) * (uint32_t)sizeof(T);
+#pragma unroll
+            for (int n = 0; n < NI; ++n) {
+                const int tr = (lw + LW * n) * RPI + lane / CPR, chunk = (lane % CPR) ^ (which ? M::v_swz(tr) : M::k_swz(tr));
+                const int kr = tr < last ? tr : last;
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(base + (uint64_t)((uint32_t)kr * pitch + chunk * 16)),
+                                                 (__attribute__((address_space(3))) void*)(own + which * TILE + (lw + LW * n) * 1024), 16, 0, 0);
+            }
+        }
+        if constexpr (MODE == SCORES_GRID) {
+            if (lw == 0) {
+#pragma unroll
+                for (int n = 0; n < KT / 32; ++n) {      // 64 floats = 32 pairs an instruction
+                    const int tr = 32 * n + (lane >> 1), kr = tr < last ? tr : last;
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p.k_coords + 2 * (int64_t)(sq.k0 + j0 + kr) + (lane & 1)),
+                                                     (__attribute__((address_space(3))) void*)(own + 2 * TILE + n * 256), 4, 0, 0);
+                }
+            }
+        }
+    };
+
+    Frag q[KS];
+    {
+        const T* src = reinterpret_cast<const T*>(p.q) + row * p.q_row + h * p.q_head + 8 * g;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) q[ks] = M::load(src + 16 * ks);
+    }
+    f32x16 o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[d][v] = 0.0f;
+    // m: the reference that exponentials are taken against, in log2 units; finite from the start, so that masked scores give zeros
+    float m = -1e30f, l = 0.0f;
+    const float scale2 = p.scale * LOG2E, cap2 = p.cap * LOG2E;
+    const float slope2 = MODE != SCORES_PLAIN && p.slopes ? p.slopes[h] * LOG2E : 0.0f;
+    f32x2 at = {0.0f, 0.0f};
+    if constexpr (MODE == SCORES_GRID) at = *reinterpret_cast<const f32x2*>(p.q_coords + 2 * row);
+    // tanh(x) for |x| < 1/4 by its series (next term 9e-9 of the value), in x^2 = y^2 / cap2^2 for the score y in log2 units
+    const float kk = MODE != SCORES_PLAIN && p.cap > 0.0f ? 1.0f / (cap2 * cap2) : 0.0f;
+    const bool series = p.cap >= 1e-3f && p.cap <= 1e15f;
+
+    auto tile_scores = [&](f32x16 (&sc)[NB], const char* tile) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sc[b][v] = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) sc[b] = M::mma(M::k_frag(tile, 32 * b + li, ks, g), q[ks], sc[b]);
+    };
+    auto shape = [&](f32x16 (&sc)[NB], const char* tile, int j0) {      // (not PLAIN) scores in log2 units
+        if (p.cap > 0.0f) {
+            float top = 0.0f;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    sc[b][v] *= scale2;
+                    top = fmaxf(top, fabsf(sc[b][v]));
+                }
+            if (series && !__any(top > 0.25f * cap2)) {
+                const float c1 = -1.0f / 3.0f * kk, c2 = 2.0f / 15.0f * kk * kk, c3 = -17.0f / 315.0f * kk * kk * kk, c4 = 62.0f / 2835.0f * kk * kk * (kk * kk);
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const float y = sc[b][v], x = y * y;
+                        sc[b][v] = y * fmaf(fmaf(fmaf(fmaf(c4, x, c3), x, c2), x, c1), x, 1.0f);
+                    }
+            } else {
+                // c tanh(y / c) = c - 2 c / (1 + e^(2 y / c))
+                const float f = 2.0f * LOG2E / cap2;
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const float y = sc[b][v], w = fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y * f)), cap2);
+                        if (sizeof(T) == 4) {
+                            const float x = y * y;           // (fp32: near zero the difference above has lost bits)
+                            const float c1 = -1.0f / 3.0f * kk, c2 = 2.0f / 15.0f * kk * kk, c3 = -17.0f / 315.0f * kk * kk * kk, c4 = 62.0f / 2835.0f * kk * kk * (kk * kk);
+                            sc[b][v] = series && fabsf(y) < 0.25f * cap2 ? y * fmaf(fmaf(fmaf(fmaf(c4, x, c3), x, c2), x, c1), x, 1.0f) : w;
+                        } else {
+                            sc[b][v] = w;
+                        }
+                    }
+            }
+        } else {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) sc[b][v] *= scale2;
+        }
+        if constexpr (MODE == SCORES_GRID) {
+            const char* c = tile + 2 * TILE + 32 * g;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {             // two keys
+                    const f32x4 to = *reinterpret_cast<const f32x4*>(c + b * 256 + (n >> 1) * 64 + (n & 1) * 16);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float dy = at[0] - to[2 * e], dx = at[1] - to[2 * e + 1];
+                        sc[b][2 * n + e] = fmaf(-slope2, __builtin_amdgcn_sqrtf(fmaf(dy, dy, dx * dx)), sc[b][2 * n + e]);
+                    }
+                }
+        } else if (p.slopes) {
+            const float d0 = (float)(place - j0 - 4 * g);
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) sc[b][v] = fmaf(-slope2, fabsf(d0 - (float)(32 * b + 8 * (v >> 2) + (v & 3))), sc[b][v]);
+        }
+    };
+    auto compute = [&](const char* stage, int t) {
+        const char* tile = stage + kw * OWN;
+        const int j0 = j_begin + t * KT;
+        if (j0 >= lim_max) return;                        // (the wave's rows see nothing of it)
+        f32x16 sc[NB];
+        tile_scores(sc, tile);
+        if constexpr (MODE != SCORES_PLAIN) shape(sc, tile, j0);
+        if (j0 + KT > lim_min || j0 + KT > j_end) {
+            const int left = (limit < j_end ? limit : j_end) - j0 - 4 * g;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (32 * b + 8 * (v >> 2) + (v & 3) >= left) sc[b][v] = -INFINITY;
+        }
+        float mx = sc[0][0];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sc[b][v]);
+        mx = halves_max(mx);
+        if constexpr (MODE == SCORES_PLAIN) mx *= scale2;
+        // the reference moves when a row's maximum has grown by more than 8: until then probabilities stay below 2^8, and the wave
+        // skips the products with the accumulators
+        const bool grow = mx > m + 8.0f;
+        if (__any(grow)) {
+            const float top = grow ? mx : m, alpha = __builtin_amdgcn_exp2f(m - top);
+            m = top;
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[d][v] *= alpha;
+        }
+        const auto values = M::values(tile + TILE, lane);
+        auto block = [&](auto ST) {                       // STEPS steps of 16 keys
+            Frag f[M::STEPS][DB];
+            M::template v_frags<decltype(ST)::value>(values, f);
+#pragma unroll
+            for (int k = 0; k < M::STEPS; ++k) {
+                constexpr int first = decltype(ST)::value;
+                float e[8];
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    const float y = sc[(first + k) >> 1][8 * ((first + k) & 1) + n];
+                    e[n] = __builtin_amdgcn_exp2f(MODE == SCORES_PLAIN ? fmaf(y, scale2, -m) : y - m);
+                    l += e[n];
+                }
+                const Frag b = M::probs(e);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) o[d] = M::mma(f[k][d], b, o[d]);
+            }
+        };
+        block(std::integral_constant<int, 0>{});
+        if constexpr (M::STEPS == 1) block(std::integral_constant<int, 1>{});
+        if constexpr (KT == 64) {
+            block(std::integral_constant<int, 2>{});
+            if constexpr (M::STEPS == 1) block(std::integral_constant<int, 3>{});
+        }
+    };
+
+    if constexpr (KW == 1) {
+        if (tiles > 0) dma(smem, 0);
+        __builtin_amdgcn_s_waitcnt(0x0F70);               // vmcnt(0): the loads into LDS have landed
+        __syncthreads();
+        for (int t = 0; t < tiles; ++t) {
+            if (t + 1 < tiles) dma(smem + ((t + 1) & 1) * STAGE, t + 1);
+            compute(smem + (t & 1) * STAGE, t);
+            __builtin_amdgcn_s_waitcnt(0x0F70);
+            __syncthreads();
+        }
+    } else {
+        // a wave's tiles are its own: it waits for its loads and for nobody
+        if (kw < tiles) dma(smem, kw);
+        int buf = 0;
+        for (int t = kw; t < tiles; t += KW, buf ^= 1) {
+            if (t + KW < tiles) {
+                dma(smem + (buf ^ 1) * STAGE, t + KW);
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * NI + (MODE == SCORES_GRID ? KT / 32 : 0)));
+            } else {
+                __builtin_amdgcn_s_waitcnt(0x0F70);
+            }
+            asm volatile("" ::: "memory");
+            compute(smem + buf * STAGE, t);
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(vmcnt_imm(63) & ~0x0F00);      // (its reads are done: the next loads may land there)
+        }
+        __syncthreads();
+    }
+    l = halves_sum(l);
+
+    // --- results.  A row is handed to attention_row if a sum of it is not finite, or nothing if it sees keys.
+    const int seen_end = limit < j_stop ? limit : j_stop;
+    if constexpr (KW == 1) {
+        float odd = l * 0.0f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) odd = fmaf(o[d][v], 0.0f, odd);
+        const bool bad = real && (odd != odd || (l == 0.0f && seen_end > j_begin));
+        uint64_t redo = __ballot(bad);
+        redo = (redo | redo >> 32) & 0xffffffffu;
+        const bool store = real && !((redo >> li) & 1);
+        const float f = grid.splits > 1 || l == 0.0f ? 1.0f : 1.0f / l;
+        if (store) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const float v[4] = {o[d][4 * n] * f, o[d][4 * n + 1] * f, o[d][4 * n + 2] * f, o[d][4 * n + 3] * f};
+                    const int c = 32 * d + 8 * n + 4 * g;
+                    if (grid.splits > 1) store_columns<4>(grid.part_o + part_row(p, row, h, split) * D + c, v);
+                    else store_columns<4>(reinterpret_cast<T*>(p.out) + row * p.out_row + h * p.out_head + c, v);
+                }
+            if (g == 0) store_stats<T>(p, grid, row, h, split, m, l);
+        }
+        for (; redo; redo &= redo - 1) {
+            const int64_t rr = r0 + qw * 32 + __builtin_ctzll(redo);
+            const int ii = (int)(rr / G);
+            attention_row<T, D>(p, grid, sq, ii, kh * G + (int)(rr - (int64_t)ii * G), j_begin, j_stop, split, lane);
+        }
+    } else {
+        // every wave leaves its sums, (c, row) 16 bytes apart by row, and its (m, l); then a thread adds four columns of a row
+        constexpr int RED = 32 * D;                       // floats of a wave's sums
+        float* sums = reinterpret_cast<float*>(smem);
+        float* ml = sums + KW * RED;
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+                *reinterpret_cast<f32x4*>(sums + kw * RED + ((8 * d + 2 * n + g) * 32 + li) * 4) = f32x4{o[d][4 * n], o[d][4 * n + 1], o[d][4 * n + 2], o[d][4 * n + 3]};
+        if (g == 0) *reinterpret_cast<f32x2*>(ml + (kw * 32 + li) * 2) = f32x2{m, l};
+        __syncthreads();
+        float w[KW], top = -1e30f, total = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KW; ++k) top = fmaxf(top, ml[(k * 32 + li) * 2]);
+#pragma unroll
+        for (int k = 0; k < KW; ++k) {
+            w[k] = __builtin_amdgcn_exp2f(ml[(k * 32 + li) * 2] - top);
+            total += w[k] * ml[(k * 32 + li) * 2 + 1];
+        }
+        const float f = grid.splits > 1 || total == 0.0f ? 1.0f : 1.0f / total;
+        float odd = total * 0.0f;
+        constexpr int PER = D / 4 / (2 * NW);             // column groups of a thread
+        f32x4 out[PER];
+#pragma unroll
+        for (int n = 0; n < PER; ++n) {
+            const int c = (2 * wave + g) + 2 * NW * n;
+            out[n] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < KW; ++k) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(sums + k * RED + (c * 32 + li) * 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[n][e] = fmaf(w[k], v[e], out[n][e]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd = fmaf(out[n][e], 0.0f, odd);
+        }
+        // a bad row is bad for all waves: they tell each other before anybody stores
+        uint32_t* flags = reinterpret_cast<uint32_t*>(ml + KW * 64);
+        uint64_t mine = __ballot(real && (odd != odd || (total == 0.0f && seen_end > j_begin)));
+        if (lane == 0) flags[wave] = (uint32_t)(mine | mine >> 32);
+        __syncthreads();
+        uint32_t redo = 0;
+#pragma unroll
+        for (int k = 0; k < NW; ++k) redo |= flags[k];
+        if (real && !((redo >> li) & 1)) {
+#pragma unroll
+            for (int n = 0; n < PER; ++n) {
+                const int c = ((2 * wave + g) + 2 * NW * n) * 4;
+                const float v[4] = {out[n][0] * f, out[n][1] * f, out[n][2] * f, out[n][3] * f};
+                if (grid.splits > 1) store_columns<4>(grid.part_o + part_row(p, row, h, split) * D + c, v);
+                else store_columns<4>(reinterpret_cast<T*>(p.out) + row * p.out_row + h * p.out_head + c, v);
+            }
+            if (wave == 0 && g == 0) store_stats<T>(p, grid, row, h, split, top, total);
+        }
+        int n = 0;
+        for (uint32_t left = __builtin_amdgcn_readfirstlane(redo); left; left &= left - 1, ++n) {
+            if (n % NW != wave) continue;
+            const int64_t rr = r0 + __builtin_ctz(left);
+            const int ii = (int)(rr / G);
+            attention_row<T, D>(p, grid, sq, ii, kh * G + (int)(rr - (int64_t)ii * G), j_begin, j_stop, split, lane);
+        }
+    }
+}
+
+// The parts of the keys put together: a wave per row and head.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void seq_attention_join_kernel(const vpe_attention_args p, const SeqAttnGrid grid) {
+    const int lane = threadIdx.x & 63;
+    const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), n_rows = (int64_t)p.q_rows * p.heads;
+    if (task >= n_rows) return;
+    const int64_t row = task / p.heads;
+    const int h = (int)(task - row * p.heads);
+    // rows of no sequence have no parts: the wave looks the row up, 64 sequences at a time
+    bool found = false;
+    for (int s0 = 0; s0 < p.sequences && !found; s0 += 64) {
+        bool in = false;
+        if (s0 + lane < p.sequences) {
+            int q0;
+            const int n = seq_rows(p, s0 + lane, q0);
+            in = row >= q0 && row < q0 + n;
+        }
+        found = __any(in);
+    }
+    if (!found) return;
+    constexpr int ND = D / 64;
+    float m = -INFINITY, l = 0.0f, acc[ND];
+#pragma unroll
+    for (int n = 0; n < ND; ++n) acc[n] = 0.0f;
+    for (int k = 0; k < grid.splits; ++k) {
+        const int64_t at = part_row(p, row, h, k);
+        const f32x2 ml = *reinterpret_cast<const f32x2*>(grid.part_ml + 2 * at);
+        if (ml[1] == 0.0f) continue;                      // (nothing of the row in this part)
+        const float top = fmaxf(m, ml[0]), a = __builtin_amdgcn_exp2f(m - top), b = __builtin_amdgcn_exp2f(ml[0] - top);
+        l = l * a + ml[1] * b;
+        m = top;
+#pragma unroll
+        for (int n = 0; n < ND; ++n) acc[n] = acc[n] * a + grid.part_o[at * D + 64 * n + lane] * b;
+    }
+#pragma unroll
+    for (int n = 0; n < ND; ++n)
+        reinterpret_cast<T*>(p.out)[row * p.out_row + h * p.out_head + 64 * n + lane] = from_f32<T>(l == 0.0f ? 0.0f : acc[n] / l);
     if (p.lse && lane == 0) p.lse[row * p.heads + h] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
 }
 

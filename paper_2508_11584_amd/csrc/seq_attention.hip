@@ -1,34 +1,79 @@
-// Instantiations and launch of the attention over packed sequences.
+// Instantiations, plan and launch of the attention over packed sequences.
+#include <algorithm>
+
 #include "operators.h"
 #include "seq_attention.h"
 
 namespace vpe {
 namespace {
 
-// A wave per row and head.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attention_rows_kernel(const vpe_attention_args p) {
-    const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int h = (int)(task % p.heads);
-    const int64_t r = task / p.heads;
-    const int i = (int)(r % p.max_q);
-    if (r / p.max_q >= p.sequences) return;
-    const Seq sq = sequence(p, (int)(r / p.max_q));
-    if (i < sq.nq) attention_row<T, D>(p, sq, i, h, threadIdx.x & 63);
+typedef void (*Kernel)(const vpe_attention_args, const SeqAttnGrid);
+// What a launch needs to know of a shape: rows of a workgroup, threads, LDS, keys that it takes at a time.
+struct Shape { Kernel kernel; int rows, threads, lds, keys; };
+
+template <typename T, int D, int KT, int QW, int KW, int MODE, int OCC>
+Shape shape() { return {&seq_attention_kernel<T, D, KT, QW, KW, MODE, OCC>, 32 * QW, 64 * QW * KW, seq_lds_bytes<T, D, KT, QW, KW, MODE>(), KT * KW}; }
+
+template <int MODE>
+Shape shape_of(int dtype, int head_dim, bool wide) {
+    if (dtype == VPE_BF16) {
+        if (head_dim == 64) return wide ? shape<bf16, 64, 64, 4, 1, MODE, 3>() : shape<bf16, 64, 32, 1, 4, MODE, 2>();
+        return wide ? shape<bf16, 128, 64, 4, 1, MODE, 2>() : shape<bf16, 128, 32, 1, 4, MODE, 1>();
+    }
+    if (head_dim == 64) return wide ? shape<float, 64, 64, 4, 1, MODE, 2>() : shape<float, 64, 32, 1, 4, MODE, 1>();
+    return wide ? shape<float, 128, 32, 4, 1, MODE, 1>() : shape<float, 128, 32, 1, 2, MODE, 1>();
 }
+Shape shape_of(const vpe_attention_args& a, const SeqAttnPlan& plan) {
+    // (a factor that is not positive turns maxima of raw scores round, a tiny one could make 0 x infinity of masked ones: LINE multiplies first)
+    if (a.q_coords) return shape_of<SCORES_GRID>(a.dtype, a.head_dim, plan.variant);
+    if (a.cap > 0.0f || a.slopes || !(a.scale > 1e-30f)) return shape_of<SCORES_LINE>(a.dtype, a.head_dim, plan.variant);
+    return shape_of<SCORES_PLAIN>(a.dtype, a.head_dim, plan.variant);
+}
+
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace
 
 SeqAttnPlan plan_seq_attention(const vpe_attention_args& a) {
-    const int64_t tasks = (int64_t)a.sequences * a.max_q * a.heads;
-    return SeqAttnPlan{0, (int)((tasks + 3) / 4 < 0x7fffffff ? (tasks + 3) / 4 : -1), 0, 1, a.max_k, 0};
+    const int G = a.heads / a.kv_heads;
+    SeqAttnPlan plan{};
+    const int64_t most = (int64_t)a.max_q * G;                    // rows of a sequence and key head
+    plan.variant = most > 32;
+    const int rows = plan.variant ? 128 : 32;
+    const int64_t direct = up(most, rows), all = (int64_t)a.q_rows * G / rows + a.sequences;
+    plan.packed = direct * a.sequences > all;
+    const int64_t blocks = plan.packed ? all : direct, base = blocks * a.kv_heads * (plan.packed ? 1 : a.sequences);
+    plan.splits = 1;
+    const int keys = 256;
+    if (base < 384) plan.splits = (int)std::min<int64_t>({512 / base, up(a.max_k, keys), 64});
+    if (plan.splits < 1) plan.splits = 1;
+    plan.per_split = (int)up(up(a.max_k, plan.splits), 128) * 128;
+    if (plan.per_split < 128) plan.per_split = 128;
+    plan.splits = (int)std::max<int64_t>(1, up(a.max_k, plan.per_split));
+    plan.blocks = base * plan.splits < 0x7fffffff ? (int)blocks : -1;
+    const uint64_t part = (uint64_t)plan.splits * a.q_rows * a.heads;
+    plan.workspace = plan.splits > 1 ? part * 4 * (a.head_dim + 2) : 0;
+    return plan;
 }
 
 hipError_t launch_seq_attention(const vpe_attention_args& a, const SeqAttnPlan& plan, hipStream_t s) {
-    typedef void (*Kernel)(const vpe_attention_args);
-    const Kernel k = a.dtype == VPE_BF16 ? (a.head_dim == 64 ? &attention_rows_kernel<bf16, 64> : &attention_rows_kernel<bf16, 128>)
-                                         : (a.head_dim == 64 ? &attention_rows_kernel<float, 64> : &attention_rows_kernel<float, 128>);
-    hipLaunchKernelGGL(k, dim3(plan.blocks), dim3(256), 0, s, a);
+    const Shape k = shape_of(a, plan);
+    SeqAttnGrid grid{plan.blocks, plan.packed, plan.splits, plan.per_split, nullptr, nullptr};
+    if (plan.splits > 1) {
+        grid.part_o = reinterpret_cast<float*>(a.workspace);
+        grid.part_ml = grid.part_o + (uint64_t)plan.splits * a.q_rows * a.heads * a.head_dim;
+    }
+    if (k.lds > 64 * 1024) {
+        const hipError_t rc = hipFuncSetAttribute(reinterpret_cast<const void*>(k.kernel), hipFuncAttributeMaxDynamicSharedMemorySize, k.lds);
+        if (rc != hipSuccess) return rc;
+    }
+    const uint32_t n = (uint32_t)plan.blocks * plan.splits * a.kv_heads * (plan.packed ? 1 : a.sequences);
+    hipLaunchKernelGGL(k.kernel, dim3(n), dim3(k.threads), k.lds, s, a, grid);
+    hipError_t rc = hipGetLastError();
+    if (rc != hipSuccess || plan.splits == 1) return rc;
+    const Kernel join = a.dtype == VPE_BF16 ? (a.head_dim == 64 ? &seq_attention_join_kernel<bf16, 64> : &seq_attention_join_kernel<bf16, 128>)
+                                            : (a.head_dim == 64 ? &seq_attention_join_kernel<float, 64> : &seq_attention_join_kernel<float, 128>);
+    hipLaunchKernelGGL(join, dim3((uint32_t)up((int64_t)a.q_rows * a.heads, 4)), dim3(256), 0, s, a, grid);
     return hipGetLastError();
 }
 
