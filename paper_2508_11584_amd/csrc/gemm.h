@@ -13,7 +13,7 @@
 namespace vpe {
 
 enum AMode { A_PLAIN = 0, A_CONV3 = 1 };
-enum Epi { EPI_STORE = 0, EPI_RESID = 1, EPI_SWIGLU = 2, EPI_QKV = 3, EPI_PATCH = 4, EPI_ROWDOT = 5 };
+enum Epi { EPI_STORE = 0, EPI_RESID = 1, EPI_SWIGLU = 2, EPI_QKV = 3, EPI_PATCH = 4, EPI_ROWDOT = 5, EPI_ADAPT = 6 };
 enum Act { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2 };
 
 // Where the tiles of a launch lie, worked out on the host (TileMap::make): the kernel's divisions by these numbers are products
@@ -45,7 +45,7 @@ struct GemmArgs {
     int a_rpi, a_istride, a_off;
     int cH, cW, cC;      // CONV3 grid and channels (K = 9 cC, cC multiple of 64)
     const void* zeros;   // CONV3: >= 16 bytes of zeros, read in place of out-of-image taps
-    int epi, act, out_f32;         // (CONV3: STORE or ROWDOT, without a folded LayerNorm; PLAIN: all but ROWDOT)
+    int epi, act, out_f32;         // (CONV3: STORE or ROWDOT, without a folded LayerNorm; PLAIN: all but ROWDOT.  ADAPT: STORE behind the rows' adapters, see below)
     void* out;           // T or float (out_f32); RESID/PATCH: float residual stream
     int64_t ldo;
     int o_rpi, o_istride, o_off;   // output row map, as for A
@@ -93,6 +93,13 @@ struct GemmArgs {
     int64_t z_a, z_w, z_out, z_bias;
     int z_inner;
     int64_t z_out2;
+    // ADAPT (plain row maps, W with N rows only): the accumulator of (row r, column c) grows by low[r] . up[adapter[r]][c], `rank` terms, ahead of
+    // bias and store; rows whose adapter lies outside 0 .. adapters - 1 stay as they are.  low [M][low_ld] in T: rank values of every row,
+    // zero up to a multiple of 16; bf16: that many upper terms, then as many lower ones (their sum is the value); up T [adapters][N][rank]
+    const int32_t* adapter;
+    const void* low;
+    const void* up;
+    int adapters, rank, low_ld;
 };
 
 // The arguments of problem blockIdx.y of a batched launch (a plain copy when the launch is not batched).

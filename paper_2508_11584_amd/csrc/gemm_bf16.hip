@@ -71,6 +71,7 @@ static bool admissible(const TileModel& c, const GemmArgs& a, int amode) {
     if (g_no_small && (c.kind == 64 || c.kind == 65)) return false;
     if (g_no_splitk && c.bm <= 64 && c.kind != 64 && c.kind != 65) return false;
     if ((c.kind == 33 || c.kind == 43) && !deep) return false;
+    if (c.kind == 384 && a.epi == EPI_ADAPT) return false;                       // (no such kernel)
     return !(c.kind == 3 && deep);
 }
 
@@ -153,7 +154,7 @@ static hipError_t launch_picked(const GemmArgs& a, int amode, hipStream_t s, int
         const int shape = conv_strip_shape(a, forced == 9, nullptr);
         if (shape) return launch_conv_strip_bf16(shape, a, s);
     }
-    if (forced && forced != 9) {
+    if (forced && forced != 9 && !(forced == 384 && a.epi == EPI_ADAPT)) {
         const bool deep = amode == A_CONV3 ? a.cC % 128 == 0 : a.K % 128 == 0;
         best = forced == 33 && !deep ? 3 : forced == 43 && !deep ? 4 : forced == 34 ? (deep ? 33 : 3) : forced;
     }

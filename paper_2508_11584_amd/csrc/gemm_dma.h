@@ -297,6 +297,74 @@ __device__ __forceinline__ void rowdot_epilogue_transposed(const GemmArgs& p, f3
     }
 }
 
+// The low-rank adapters of a wave tile's rows (EPI_ADAPT), added to its accumulators: a block of 32 rows at a time, for every adapter that
+// its rows have: the adapter's products are taken for all 32 rows and added to those that have it, by selection, so that an adapter's
+// infinities and NaN stay with its rows.  Operands come
+// straight from global memory: a lane has a row's, or a column's, eight elements of a 16-deep step.  (A tile of one adapter of rank 32 and
+// 256 x 256 takes 1.5 us for it, all latency: three dependent loads.)
+template <typename T, int MI, int NI>
+__device__ __forceinline__ void adapter_steps(const GemmArgs& p, f32x16 (&acc)[MI][NI], int row0, int col0, int lane) {
+    const int g = lane >> 5, li = lane & 31, steps = (p.rank + 15) >> 4;
+    struct Frag { f32x4 lo, hi; };                       // fp32: a step's eight elements; bf16 (lo alone): 16 bytes
+    auto load = [&](const T* src) {
+        Frag f;
+        f.lo = *reinterpret_cast<const f32x4*>(src);
+        if (sizeof(T) == 4) f.hi = *reinterpret_cast<const f32x4*>(src + 4);
+        return f;
+    };
+    const T* up[NI];
+    auto columns = [&](int a) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const int c = col0 + 32 * j + li;
+            up[j] = reinterpret_cast<const T*>(p.up) + ((int64_t)a * p.N + (c < p.N ? c : p.N - 1)) * p.rank + 8 * g;
+        }
+    };
+    auto multiply = [&](const Frag& b, const Frag& t, const Frag& t2, f32x16 c) {
+        if constexpr (sizeof(T) == 2) {
+            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b.lo), __builtin_bit_cast(bf16x8, t2.lo), c, 0, 0, 0);
+            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, b.lo), __builtin_bit_cast(bf16x8, t.lo), c, 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(b.lo[e], t.lo[e], c, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(b.hi[e], t.hi[e], c, 0, 0, 0);
+        }
+        return c;
+    };
+    const Frag zero = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
+    if (p.adapters == 0) return;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const int r = row0 + 32 * i + li < p.M ? row0 + 32 * i + li : p.M - 1;
+        const int id = p.adapter[r];
+        const T* low = reinterpret_cast<const T*>(p.low) + (int64_t)r * p.low_ld + 8 * g;
+        uint64_t todo = __ballot(id >= 0 && id < p.adapters);
+        while (todo) {
+            const int a = __builtin_amdgcn_readlane(id, __builtin_ctzll(todo));
+            const bool mine = id == a;
+            const uint64_t rows = __ballot(mine);
+            todo &= ~rows;
+            columns(a);
+            // (a block's products in registers of their own: with the accumulators themselves carried through the step loop the compiler
+            // keeps those of the large tiles in scratch)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                f32x16 c;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) c[v] = 0.0f;
+#pragma unroll 1
+                for (int ks = 0; ks < steps; ++ks) {
+                    const bool there = 16 * ks + 8 * g < p.rank;           // (a rank that is an odd multiple of eight ends in half a step)
+                    c = multiply(there ? load(up[j] + 16 * ks) : zero, load(low + 16 * ks), sizeof(T) == 2 ? load(low + 16 * (steps + ks)) : zero, c);
+                }
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[i][j][v] = mine ? acc[i][j][v] + c[v] : acc[i][j][v];
+            }
+        }
+    }
+}
+
 // BM x BN tiles, BK elements per k-tile (LDS rows of 64, 128 or 256 bytes), S LDS stages: the loads of tile kt + S - 1 are
 // in flight while tile kt is multiplied, so a load has S - 1 tile times to arrive.  WGM x WGN waves share a tile (BM / WGM
 // rows and BN / WGN columns each); OCC workgroups per CU (the launch bound is in waves per SIMD: OCC * waves / 4).
@@ -368,7 +436,8 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, OCC * WGM * WGN * KG / 4) void
     for (int s = 0; s < B_SLOTS; ++s) {
         const int row = (wave + NW * s) * RPI + lane / CPR;
         const int c = (lane % CPR) ^ ((row >> SW_SHIFT) & SW_MASK);
-        boff[s] = (row * p.K + c * CE) * ESZ;
+        const int wr = EPI == EPI_ADAPT && row > p.N - 1 - n0 ? p.N - 1 - n0 : row;       // (a caller's weight ends with its last row)
+        boff[s] = (wr * p.K + c * CE) * ESZ;
     }
     const char* zptr = reinterpret_cast<const char*>(p.zeros);
 
@@ -675,12 +744,15 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, OCC * WGM * WGN * KG / 4) void
             }
         }
     }
+    constexpr int OUT = EPI == EPI_ADAPT ? EPI_STORE : EPI;
+    if constexpr (EPI == EPI_ADAPT)
+        if (kg == 0) adapter_steps<T, MI, NI>(p, acc, m0 + wm * WM, n0 + wn * WN, lane);
     if constexpr (BLOCK) {                                    // (whole tile staged in LDS)
-        block_epilogue<T, EPI, BM, BN, WGM, WGN, KG, AMODE == A_PLAIN>(p, acc, smem, lnrow, m0, n0);
+        block_epilogue<T, OUT, BM, BN, WGM, WGN, KG, AMODE == A_PLAIN && EPI != EPI_ADAPT>(p, acc, smem, lnrow, m0, n0);
     } else if constexpr (EPI == EPI_ROWDOT) {
         rowdot_epilogue_transposed<MI, NI, WM, WN, BN, 64 * NW, false>(p, acc, smem, wm, wn, tid, m0, n0);
     } else {
-        wave_tile_epilogue<T, EPI, BM, MI, NI, WM, WN, AMODE == A_PLAIN>(p, acc, smem, lnrow, wave, wm, wn, tid, m0, n0);
+        wave_tile_epilogue<T, OUT, BM, MI, NI, WM, WN, AMODE == A_PLAIN && EPI != EPI_ADAPT>(p, acc, smem, lnrow, wave, wm, wn, tid, m0, n0);
     }
 }
 
@@ -694,12 +766,13 @@ static inline hipError_t launch_gemm_dma(const GemmArgs& a, int amode, hipStream
     typedef void (*Kernel)(const GemmArgs);
     // (tiles of 32 columns: the residual epilogue only)
     constexpr auto kernel_for = [](auto mode, auto epi) -> Kernel {
-        if constexpr (BN % 64 && !(mode == A_PLAIN && epi == EPI_RESID)) return nullptr;
+        // (384-row tiles have no registers left for adapters: 192 accumulators)
+        if constexpr ((BN % 64 && !(mode == A_PLAIN && epi == EPI_RESID)) || (BM == 384 && epi == EPI_ADAPT)) return nullptr;
         else return &gemm_dma_kernel<T, BN, BK, S, WGM, WGN, OCC, decltype(mode)::value, decltype(epi)::value, BM, KG, RING>;
     };
 #define VPE_KERNEL(mode, epi) kernel_for(std::integral_constant<int, mode>{}, std::integral_constant<int, epi>{})
     static const Kernel plain[] = {VPE_KERNEL(A_PLAIN, EPI_STORE), VPE_KERNEL(A_PLAIN, EPI_RESID), VPE_KERNEL(A_PLAIN, EPI_SWIGLU),
-                                   VPE_KERNEL(A_PLAIN, EPI_QKV), VPE_KERNEL(A_PLAIN, EPI_PATCH)};
+                                   VPE_KERNEL(A_PLAIN, EPI_QKV), VPE_KERNEL(A_PLAIN, EPI_PATCH), VPE_KERNEL(A_PLAIN, EPI_ADAPT)};
     static const Kernel conv[] = {VPE_KERNEL(A_CONV3, EPI_STORE), VPE_KERNEL(A_CONV3, EPI_ROWDOT)};
 #undef VPE_KERNEL
     static bool configured = false;
@@ -715,8 +788,8 @@ static inline hipError_t launch_gemm_dma(const GemmArgs& a, int amode, hipStream
     }
     if (configure_only) return hipSuccess;
     if (a.K < BK || a.K % BK || (amode == A_CONV3 && a.cC % BK)) return hipErrorInvalidValue;      // the k loop has no remainder
-    if (amode == A_CONV3 ? a.epi != EPI_STORE && a.epi != EPI_ROWDOT : a.epi < EPI_STORE || a.epi > EPI_PATCH) return hipErrorInvalidValue;
-    const Kernel k = amode == A_CONV3 ? conv[a.epi == EPI_ROWDOT] : plain[a.epi];
+    if (amode == A_CONV3 ? a.epi != EPI_STORE && a.epi != EPI_ROWDOT : a.epi < EPI_STORE || (a.epi > EPI_PATCH && a.epi != EPI_ADAPT)) return hipErrorInvalidValue;
+    const Kernel k = amode == A_CONV3 ? conv[a.epi == EPI_ROWDOT] : plain[a.epi == EPI_ADAPT ? 5 : a.epi];
     if (!k) return hipErrorInvalidValue;
     GemmArgs args = a;
     args.map = TileMap::make(cdiv(a.M - a.m_begin, BM), cdiv(a.N, BN));

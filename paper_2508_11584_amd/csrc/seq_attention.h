@@ -37,6 +37,16 @@ struct SeqAttnGrid {
     float *part_o, *part_ml;     // splits > 1: [split][q_rows][heads][D] sums against the part's reference, [split][q_rows][heads][2] (reference, sum)
 };
 
+// A kernel's argument at `offset`, read from its argument segment where this stands.
+template <typename A>
+__device__ __forceinline__ A kernel_args(int offset) {
+    auto base = (const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(base));
+    A a;
+    __builtin_memcpy(&a, (const char*)(base + offset), sizeof a);
+    return a;
+}
+
 // Keys that the row at `place` sees: 0 .. limit - 1.  (Causal rows see what is before them and the prefix: one range.)
 __device__ __forceinline__ int key_limit(const vpe_attention_args& p, const Seq& sq, int place) {
     if (!p.causal) return sq.nk;
@@ -431,6 +441,7 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
                             const float x = y * y;           // (fp32: near zero the difference above has lost bits)
                             const float c1 = -1.0f / 3.0f * kk, c2 = 2.0f / 15.0f * kk * kk, c3 = -17.0f / 315.0f * kk * kk * kk, c4 = 62.0f / 2835.0f * kk * kk * (kk * kk);
                             sc[b][v] = series && fabsf(y) < 0.25f * cap2 ? y * fmaf(fmaf(fmaf(fmaf(c4, x, c3), x, c2), x, c1), x, 1.0f) : w;
+                            if ((v & 3) == 3) __builtin_amdgcn_sched_barrier(0);      // (comparisons of a whole tile at once have no scalar registers)
                         } else {
                             sc[b][v] = w;
                         }
@@ -555,7 +566,9 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
     }
     l = halves_sum(l);
 
-    // --- results.  A row is handed to attention_row if a sum of it is not finite, or nothing if it sees keys.
+    // --- results.  A row is handed to attention_row if a sum of it is not finite, or nothing if it sees keys.  (The arguments are read once
+    // more from the kernel's own segment: what only this part needs holds no scalar registers through the loop.)
+    auto leave = [&](const vpe_attention_args& p, const SeqAttnGrid& grid) {
     const int seen_end = limit < j_stop ? limit : j_stop;
     if constexpr (KW == 1) {
         float odd = l * 0.0f;
@@ -649,6 +662,8 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
             attention_row<T, D>(p, grid, sq, ii, kh * G + (int)(rr - (int64_t)ii * G), j_begin, j_stop, split, lane);
         }
     }
+    };
+    leave(kernel_args<vpe_attention_args>(0), kernel_args<SeqAttnGrid>(sizeof(vpe_attention_args)));
 }
 
 // The parts of the keys put together: a wave per row and head.

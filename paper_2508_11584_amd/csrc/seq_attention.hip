@@ -20,7 +20,8 @@ Shape shape_of(int dtype, int head_dim, bool wide) {
         if (head_dim == 64) return wide ? shape<bf16, 64, 64, 4, 1, MODE, 3>() : shape<bf16, 64, 32, 1, 4, MODE, 2>();
         return wide ? shape<bf16, 128, 64, 4, 1, MODE, 2>() : shape<bf16, 128, 32, 1, 4, MODE, 1>();
     }
-    if (head_dim == 64) return wide ? shape<float, 64, 64, 4, 1, MODE, 2>() : shape<float, 64, 32, 1, 4, MODE, 1>();
+    // (with coordinates 64 keys at a time take a register too many)
+    if (head_dim == 64) return wide ? shape<float, 64, MODE == SCORES_GRID ? 32 : 64, 4, 1, MODE, 2>() : shape<float, 64, 32, 1, 4, MODE, 1>();
     return wide ? shape<float, 128, 32, 4, 1, MODE, 1>() : shape<float, 128, 32, 1, 2, MODE, 1>();
 }
 Shape shape_of(const vpe_attention_args& a, const SeqAttnPlan& plan) {

@@ -655,3 +655,14 @@ def test_a_block_for_packed_requests(dtype):
     bound = 5.0 * HALF_BF16 if dtype == "bf16" else 8.0 * walk(D)
     assert torch.equal(x1, x)
     assert rel(y, ry) < bound and rel(x2, r2) < bound and rel(h2, rn) < bound
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [2, 300])
+def test_adapters_write_unaligned_results(rows, dtype):
+    """out begins at any element, with rows a multiple of 16 bytes apart."""
+    x, w, kw = adapter_case(rows, 128, 264, 16, 2, dtype, "mixed")
+    for first in (1, 2, 5):
+        flat = torch.full((rows * 272 + 8,), 7.0, dtype=x.dtype, device="cuda")
+        check_adapters(x, w, out=flat[first:first + rows * 272].view(rows, 272)[:, :264], **kw)
+        assert int((flat == 7.0).sum()) >= flat.numel() - rows * 264
