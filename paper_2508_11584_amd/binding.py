@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from struct import Struct
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -101,10 +102,10 @@ def load_library(path: Optional[str] = None):
     L.vpe_stats.argtypes = [vp, i64p, i64p, i64p, i32]
     L.vpe_time_kernel.argtypes = [vp, i32, i32, C.POINTER(C.c_float), C.POINTER(C.c_double), C.POINTER(C.c_double)]
     L.vpe_attention_workspace_bytes.argtypes = [C.POINTER(vpe_attention_args), C.POINTER(C.c_uint64)]
-    L.vpe_attention.argtypes = [C.POINTER(vpe_attention_args), vp]
-    L.vpe_block_norm.argtypes = [C.POINTER(vpe_block_norm_args), vp]
+    L.vpe_attention.argtypes = [vp, vp]              # (a struct by reference, or its packed bytes)
+    L.vpe_block_norm.argtypes = [vp, vp]              # (a struct by reference, or its packed bytes)
     L.vpe_adapter_linear_workspace_bytes.argtypes = [C.POINTER(vpe_adapter_linear_args), C.POINTER(C.c_uint64)]
-    L.vpe_adapter_linear.argtypes = [C.POINTER(vpe_adapter_linear_args), vp]
+    L.vpe_adapter_linear.argtypes = [vp, vp]              # (a struct by reference, or its packed bytes)
     L.vpe_last_error.argtypes = [vp]
     L.vpe_last_error.restype = C.c_char_p
     L.vpe_destroy.argtypes = [vp]
@@ -173,76 +174,109 @@ def preprocess_u8(frames, out, mean, std, stream=None) -> None:
 
 
 # ------------------------------------------------------------------ operators on packed rows
-def _raw_stream(stream) -> Optional[int]:
-    """A torch stream, a raw hipStream_t as int, or None (the default stream)."""
-    return None if stream is None else stream if isinstance(stream, int) else stream.cuda_stream
+# A call takes some microseconds on the device: its arguments are packed in one go (the layouts are those of the structs above) and the
+# tensors are looked at as little as the checks allow.
+_PACK_ATTENTION = Struct("10i2f4Q8q9QQ")
+_PACK_BLOCK_NORM = Struct("6i2f4Q4q9Q")
+_PACK_ADAPTER = Struct("7i4x4Q2q5QQ")
+assert (_PACK_ATTENTION.size, _PACK_BLOCK_NORM.size, _PACK_ADAPTER.size) == tuple(
+    C.sizeof(t) for t in (vpe_attention_args, vpe_block_norm_args, vpe_adapter_linear_args))
+
+
+def _refuse(message: str):
+    raise VpeError(VPE_EINVAL, message)
+
+
+def _types():
+    """torch and its type objects, once torch is wanted."""
+    global _torch, _f32, _bf16, _i32, _u8
+    if _torch is None:
+        import torch
+        _f32, _bf16, _i32, _u8, _torch = torch.float32, torch.bfloat16, torch.int32, torch.uint8, torch
+    return _torch
+
+
+_torch = _f32 = _bf16 = _i32 = _u8 = None
 
 
 def _dtype_of(t) -> int:
-    import torch
-    if t.dtype not in (torch.bfloat16, torch.float32):
-        raise VpeError(VPE_EINVAL, f"tensors must be bfloat16 or float32, not {t.dtype}")
-    return VPE_BF16 if t.dtype == torch.bfloat16 else VPE_F32
+    d = t.dtype
+    if d is _bf16:
+        return VPE_BF16
+    if d is _f32:
+        return VPE_F32
+    _refuse(f"tensors must be bfloat16 or float32, not {d}")
 
 
-def _device_ptr(name: str, t, device, dtype=None, shape=None, contiguous=True) -> Optional[int]:
-    """The address of a tensor that a call is to use, or None for None; what does not fit is refused."""
+def _ptr(name: str, t, index: int, dtype, shape) -> int:
+    """The address of a contiguous tensor that a call is to use, 0 for None; what does not fit is refused."""
     if t is None:
-        return None
-    if dtype is not None and t.dtype != dtype:
-        raise VpeError(VPE_EINVAL, f"{name} must be {dtype}, not {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise VpeError(VPE_EINVAL, f"{name} has the shape {tuple(t.shape)}, {tuple(shape)} expected")
-    if contiguous and not t.is_contiguous():
-        raise VpeError(VPE_EINVAL, f"{name} must be contiguous")
-    if t.device != device:
-        raise VpeError(VPE_EINVAL, f"{name} is on {t.device}, {device} expected")
+        return 0
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != index:
+        _refuse(f"{name}: contiguous {dtype} {tuple(shape)} on device {index} expected, not {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _workspace(args, workspace, device) -> None:
-    import torch
-    if workspace is None:
-        return
-    if workspace.dtype != torch.uint8:
-        raise VpeError(VPE_EINVAL, "workspace must be a uint8 tensor")
-    args.workspace = _device_ptr("workspace", workspace, device)
-    args.workspace_bytes = workspace.numel()
+def _workspace(t, index: int):
+    if t is None:
+        return 0, 0
+    if t.dtype is not _u8 or not t.is_contiguous() or t.get_device() != index:
+        _refuse("workspace must be a contiguous uint8 tensor on the tensors' device")
+    return t.data_ptr(), t.numel()
 
 
-def _enqueue(call, args, device, stream) -> None:
-    """Makes the call with the tensors' device current."""
-    import torch
-    if device.type != "cuda":
-        raise VpeError(VPE_EINVAL, f"tensors are on {device}: device memory required")
-    with torch.cuda.device(device):
-        rc = call(C.byref(args), _raw_stream(stream))
+def _enqueue(call, packed: bytes, index: int, stream) -> None:
+    """Makes the call with the tensors' device current; stream: a torch stream, a raw hipStream_t as int, or None (the default stream)."""
+    if index < 0:
+        _refuse("tensors must be in device memory")
+    raw = None if stream is None else stream if isinstance(stream, int) else stream.cuda_stream
+    if _torch.cuda.current_device() == index:
+        rc = call(packed, raw)
+    else:
+        with _torch.cuda.device(index):
+            rc = call(packed, raw)
     if rc:
         raise VpeError(rc, vpe_last_error(None))
 
 
 def _row_stride(name: str, t) -> int:
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise VpeError(VPE_EINVAL, f"{name} must be a matrix with contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])      # (the stride of a single row says nothing)
+    rows, cols = t.shape
+    stride = t.stride()
+    if cols > 1 and stride[1] != 1:
+        _refuse(f"{name} must be a matrix with contiguous rows")
+    return stride[0] if rows > 1 else max(stride[0], cols)            # (the stride of a single row says nothing)
 
 
-def _attention_sizes(q, k, sequences: int, max_q: int, max_k: int) -> vpe_attention_args:
-    if q.dim() != 3 or k.dim() != 3 or q.shape[2] != k.shape[2] or q.dtype != k.dtype:
-        raise VpeError(VPE_EINVAL, "q and k must be [rows, heads, head_dim] of one type and head_dim")
-    a = vpe_attention_args()
-    a.dtype, a.heads, a.kv_heads, a.head_dim = _dtype_of(q), q.shape[1], k.shape[1], q.shape[2]
-    a.sequences, a.max_q, a.max_k, a.q_rows, a.k_rows = sequences, max_q, max_k, q.shape[0], k.shape[0]
-    return a
+def _attention_sizes(q, k):
+    _types()
+    if q.dim() != 3 or k.dim() != 3 or q.dtype is not k.dtype:
+        _refuse("q and k must be [rows, heads, head_dim] of one type")
+    (q_rows, heads, head_dim), (k_rows, kv_heads, k_dim) = q.shape, k.shape
+    if head_dim != k_dim:
+        _refuse("q and k must have the same head_dim")
+    return _dtype_of(q), q_rows, heads, head_dim, k_rows, kv_heads
 
 
 def attention_workspace_bytes(q, k, *, sequences: int, max_q: int, max_k: int) -> int:
     """Bytes of workspace that `attention` needs for tensors of these shapes, whatever the offsets say."""
-    a, out = _attention_sizes(q, k, sequences, max_q, max_k), C.c_uint64(0)
+    a, out = vpe_attention_args(), C.c_uint64(0)
+    a.dtype, a.q_rows, a.heads, a.head_dim, a.k_rows, a.kv_heads = _attention_sizes(q, k)
+    a.sequences, a.max_q, a.max_k = sequences, max_q, max_k
     rc = lib().vpe_attention_workspace_bytes(C.byref(a), C.byref(out))
     if rc:
         raise VpeError(rc, vpe_last_error(None))
     return int(out.value)
+
+
+def _heads_matrix(name: str, t, shape, dtype, index: int):
+    """(address, stride of the rows, of the heads) of a [rows, heads, head_dim] tensor."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        _refuse(f"{name}: {dtype} {tuple(shape)} on device {index} expected, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    row, head, last = t.stride()
+    rows, heads, dim = shape
+    if last != 1 and rows:
+        _refuse(f"{name}'s last axis must be contiguous")
+    return t.data_ptr(), row if rows > 1 else heads * dim, head if heads > 1 else dim       # (the stride of an axis of length one says nothing)
 
 
 def attention(q, k, v, out, *, q_offsets, k_offsets, max_q: int, max_k: int, k_lengths=None, causal: bool = False, prefix=None,
@@ -253,31 +287,30 @@ def attention(q, k, v, out, *, q_offsets, k_offsets, max_q: int, max_k: int, k_l
     [sequences]; slopes float32 [heads]; coordinates float32 [rows, 2]; lse float32 [q_rows, heads] (written, as is out).
     scale: 1 / sqrt(head_dim) if not given.  workspace: a uint8 tensor of attention_workspace_bytes.  stream: a torch stream, a raw
     hipStream_t as int, or None (the default stream)."""
-    import torch
-    sequences = q_offsets.numel() - 1
-    a = _attention_sizes(q, k, sequences, max_q, max_k)
-    dev, heads = q.device, a.heads
-    if v.shape != k.shape or out.shape != q.shape:
-        raise VpeError(VPE_EINVAL, "v must have k's shape, out q's")
-    for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
-        if t.stride(2) != 1 and t.numel():
-            raise VpeError(VPE_EINVAL, f"{name}'s last axis must be contiguous")
-        setattr(a, name, _device_ptr(name, t, dev, q.dtype, contiguous=False))
-        # (the stride of an axis of length one says nothing)
-        setattr(a, name + "_row", t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2])
-        setattr(a, name + "_head", t.stride(1) if t.shape[1] > 1 else t.shape[2])
-    a.causal, a.scale, a.cap = int(bool(causal)), q.shape[2] ** -0.5 if scale is None else scale, cap
-    i32, f32 = torch.int32, torch.float32
-    a.q_offsets = _device_ptr("q_offsets", q_offsets, dev, i32, (sequences + 1,))
-    a.k_offsets = _device_ptr("k_offsets", k_offsets, dev, i32, (sequences + 1,))
-    a.k_lengths = _device_ptr("k_lengths", k_lengths, dev, i32, (sequences,))
-    a.prefix = _device_ptr("prefix", prefix, dev, i32, (sequences,))
-    a.slopes = _device_ptr("slopes", slopes, dev, f32, (heads,))
-    a.q_coords = _device_ptr("q_coords", q_coords, dev, f32, (q.shape[0], 2))
-    a.k_coords = _device_ptr("k_coords", k_coords, dev, f32, (k.shape[0], 2))
-    a.lse = _device_ptr("lse", lse, dev, f32, (q.shape[0], heads))
-    _workspace(a, workspace, dev)
-    _enqueue(lib().vpe_attention, a, dev, stream)
+    dtype, q_rows, heads, head_dim, k_rows, kv_heads = _attention_sizes(q, k)
+    dev, sequences, q_shape, k_shape = q.get_device(), q_offsets.numel() - 1, q.shape, k.shape
+    qp, q_row, q_head = _heads_matrix("q", q, q_shape, q.dtype, dev)
+    kp, k_row, k_head = _heads_matrix("k", k, k_shape, q.dtype, dev)
+    vp, v_row, v_head = _heads_matrix("v", v, k_shape, q.dtype, dev)
+    op, o_row, o_head = _heads_matrix("out", out, q_shape, q.dtype, dev)
+    ends, each = (sequences + 1,), (sequences,)
+    wp, wb = _workspace(workspace, dev)
+    packed = _PACK_ATTENTION.pack(
+        dtype, heads, kv_heads, head_dim, sequences, max_q, max_k, q_rows, k_rows, 1 if causal else 0, head_dim ** -0.5 if scale is None else scale, cap,
+        qp, kp, vp, op, q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, _ptr("q_offsets", q_offsets, dev, _i32, ends),
+        _ptr("k_offsets", k_offsets, dev, _i32, ends), _ptr("k_lengths", k_lengths, dev, _i32, each), _ptr("prefix", prefix, dev, _i32, each),
+        _ptr("slopes", slopes, dev, _f32, (heads,)), _ptr("q_coords", q_coords, dev, _f32, (q_rows, 2)),
+        _ptr("k_coords", k_coords, dev, _f32, (k_rows, 2)), _ptr("lse", lse, dev, _f32, (q_rows, heads)), wp, wb)
+    _enqueue(lib().vpe_attention, packed, dev, stream)
+
+
+def _matrix(name: str, t, shape, dtype, index: int):
+    """(address, stride of the rows) of a matrix whose rows may be strided, zeros for None."""
+    if t is None:
+        return 0, 0
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
+        _refuse(f"{name}: {dtype} {tuple(shape)} on device {index} expected, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr(), _row_stride(name, t)
 
 
 def block_norm(x, out, *, branch=None, normed=None, post: int = VPE_NORM_NONE, post_gain=None, post_bias=None, pre: int = VPE_NORM_NONE,
@@ -286,41 +319,46 @@ def block_norm(x, out, *, branch=None, normed=None, post: int = VPE_NORM_NONE, p
     """vpe_block_norm on torch CUDA tensors: x, out float32 [rows, dim] (out is written and may be x); branch, normed [rows, dim],
     bfloat16 or float32 (normed is written); gains, biases and layer_scale float32 [dim]; gate, scale, shift float32 [requests, dim];
     request int32 [rows].  Rows may be strided.  stream: as for attention."""
-    import torch
-    a, dev, (rows, dim) = vpe_block_norm_args(), x.device, x.shape
-    typed = [t for t in (branch, normed) if t is not None]
-    a.dtype = _dtype_of(typed[0]) if typed else VPE_F32
-    for name, t, dtype in (("x", x, torch.float32), ("out", out, torch.float32), ("branch", branch, None), ("normed", normed, None)):
-        if t is None:
-            continue
-        setattr(a, name, _device_ptr(name, t, dev, dtype or typed[0].dtype, (rows, dim), contiguous=False))
-        setattr(a, name + "_row", _row_stride(name, t))
-    modulation = [t for t in (gate, scale, shift) if t is not None]
-    a.rows, a.dim, a.requests = rows, dim, modulation[0].shape[0] if modulation else 0
-    a.post, a.pre, a.residual_scale, a.eps = post, pre, residual_scale, eps
-    for name, t in (("post_gain", post_gain), ("post_bias", post_bias), ("pre_gain", pre_gain), ("pre_bias", pre_bias), ("layer_scale", layer_scale)):
-        setattr(a, name, _device_ptr(name, t, dev, torch.float32, (dim,)))
-    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
-        setattr(a, name, _device_ptr(name, t, dev, torch.float32, (a.requests, dim)))
-    a.request = _device_ptr("request", request, dev, torch.int32, (rows,))
-    _enqueue(lib().vpe_block_norm, a, dev, stream)
+    _types()
+    if x.dim() != 2:
+        _refuse("x must be a matrix")
+    shape, dev = x.shape, x.get_device()
+    rows, dim = shape
+    typed = branch if branch is not None else normed
+    dtype, t = (VPE_F32, _f32) if typed is None else (_dtype_of(typed), typed.dtype)
+    xp, x_row = _matrix("x", x, shape, _f32, dev)
+    op, out_row = _matrix("out", out, shape, _f32, dev)
+    bp, branch_row = _matrix("branch", branch, shape, t, dev)
+    np_, normed_row = _matrix("normed", normed, shape, t, dev)
+    table = gate if gate is not None else scale if scale is not None else shift
+    requests = 0 if table is None else table.shape[0]
+    vector, modulation = (dim,), (requests, dim)
+    packed = _PACK_BLOCK_NORM.pack(
+        dtype, rows, dim, requests, post, pre, residual_scale, eps, xp, bp, op, np_, x_row, branch_row, out_row, normed_row,
+        _ptr("post_gain", post_gain, dev, _f32, vector), _ptr("post_bias", post_bias, dev, _f32, vector), _ptr("pre_gain", pre_gain, dev, _f32, vector),
+        _ptr("pre_bias", pre_bias, dev, _f32, vector), _ptr("layer_scale", layer_scale, dev, _f32, vector), _ptr("gate", gate, dev, _f32, modulation),
+        _ptr("scale", scale, dev, _f32, modulation), _ptr("shift", shift, dev, _f32, modulation), _ptr("request", request, dev, _i32, (rows,)))
+    _enqueue(lib().vpe_block_norm, packed, dev, stream)
 
 
-def _adapter_sizes(x, weight, a_) -> vpe_adapter_linear_args:
-    if x.dim() != 2 or weight.dim() != 2 or x.shape[1] != weight.shape[1] or x.dtype != weight.dtype:
-        raise VpeError(VPE_EINVAL, "x must be [rows, in_features], weight [out_features, in_features] of one type")
-    p = vpe_adapter_linear_args()
-    p.dtype, p.rows, p.in_features, p.out_features = _dtype_of(x), x.shape[0], x.shape[1], weight.shape[0]
-    if a_ is not None:
-        if a_.dim() != 3 or a_.shape[2] != x.shape[1]:
-            raise VpeError(VPE_EINVAL, "a must be [adapters, rank, in_features]")
-        p.adapters, p.rank = a_.shape[0], a_.shape[1]
-    return p
+def _adapter_sizes(x, weight, a):
+    _types()
+    if x.dim() != 2 or weight.dim() != 2 or x.dtype is not weight.dtype:
+        _refuse("x must be [rows, in_features], weight [out_features, in_features] of one type")
+    (rows, in_features), (out_features, columns) = x.shape, weight.shape
+    if in_features != columns:
+        _refuse("weight must be [out_features, in_features]")
+    if a is None:
+        return _dtype_of(x), rows, in_features, out_features, 0, 0
+    if a.dim() != 3 or a.shape[2] != in_features:
+        _refuse("a must be [adapters, rank, in_features]")
+    return _dtype_of(x), rows, in_features, out_features, a.shape[0], a.shape[1]
 
 
 def adapter_linear_workspace_bytes(x, weight, a=None) -> int:
     """Bytes of workspace that `adapter_linear` needs for tensors of these shapes."""
-    p, out = _adapter_sizes(x, weight, a), C.c_uint64(0)
+    p, out = vpe_adapter_linear_args(), C.c_uint64(0)
+    p.dtype, p.rows, p.in_features, p.out_features, p.adapters, p.rank = _adapter_sizes(x, weight, a)
     rc = lib().vpe_adapter_linear_workspace_bytes(C.byref(p), C.byref(out))
     if rc:
         raise VpeError(rc, vpe_last_error(None))
@@ -332,24 +370,19 @@ def adapter_linear(x, weight, out, *, bias=None, a=None, b=None, adapter=None, s
     a [adapters, rank, in_features], b [adapters, out_features, rank], all bfloat16 or all float32; out [rows, out_features] of
     that type or float32 (written); bias float32 [out_features]; adapter int32 [rows] (outside 0 .. adapters - 1: none); scale float32
     [adapters].  workspace: a uint8 tensor of adapter_linear_workspace_bytes.  stream: as for attention."""
-    import torch
-    p, dev = _adapter_sizes(x, weight, a), x.device
+    dtype, rows, in_features, out_features, adapters, rank = _adapter_sizes(x, weight, a)
     if (a is None) != (b is None) or (a is None) != (adapter is None):
-        raise VpeError(VPE_EINVAL, "a, b and adapter go together")
-    if out.dtype not in (x.dtype, torch.float32):
-        raise VpeError(VPE_EINVAL, f"out must be {x.dtype} or float32, not {out.dtype}")
-    p.out_f32 = int(out.dtype == torch.float32)
-    p.x = _device_ptr("x", x, dev, contiguous=False)
-    p.out = _device_ptr("out", out, dev, shape=(x.shape[0], weight.shape[0]), contiguous=False)
-    p.x_row, p.out_row = _row_stride("x", x), _row_stride("out", out)
-    p.weight = _device_ptr("weight", weight, dev)
-    p.bias = _device_ptr("bias", bias, dev, torch.float32, (weight.shape[0],))
-    p.a = _device_ptr("a", a, dev, x.dtype)
-    p.b = _device_ptr("b", b, dev, x.dtype, (p.adapters, weight.shape[0], p.rank))
-    p.adapter = _device_ptr("adapter", adapter, dev, torch.int32, (x.shape[0],))
-    p.scale = _device_ptr("scale", scale, dev, torch.float32, (p.adapters,))
-    _workspace(p, workspace, dev)
-    _enqueue(lib().vpe_adapter_linear, p, dev, stream)
+        _refuse("a, b and adapter go together")
+    dev, t = x.get_device(), x.dtype
+    out_f32 = out.dtype is _f32
+    xp, x_row = _matrix("x", x, x.shape, t, dev)
+    op, out_row = _matrix("out", out, (rows, out_features), _f32 if out_f32 else t, dev)
+    wp, wb = _workspace(workspace, dev)
+    packed = _PACK_ADAPTER.pack(
+        dtype, 1 if out_f32 else 0, rows, in_features, out_features, adapters, rank, xp, _ptr("weight", weight, dev, t, weight.shape),
+        _ptr("bias", bias, dev, _f32, (out_features,)), op, x_row, out_row, _ptr("a", a, dev, t, (adapters, rank, in_features)),
+        _ptr("b", b, dev, t, (adapters, out_features, rank)), _ptr("adapter", adapter, dev, _i32, (rows,)), _ptr("scale", scale, dev, _f32, (adapters,)), wp, wb)
+    _enqueue(lib().vpe_adapter_linear, packed, dev, stream)
 
 
 def vpe_next_encode_stream(engine) -> Optional[int]:
