@@ -10,11 +10,14 @@ namespace vpe {
 
 // Launch plan of an attention call: a function of its sizes alone, so that workspace and grid agree whatever the arrays hold.
 struct SeqAttnPlan {
-    int variant;         // workgroup shape (seq_attention.hip)
-    int blocks;          // row blocks of the longest possible sequence, or of all sequences together (`packed`)
+    int rows;            // rows of a workgroup: 128 (four waves of 32) or 32 (four waves that share the keys)
+    int blocks;          // row blocks of the longest possible sequence, or of all sequences together (`packed`); -1: too many for a launch
     int packed;          // 1: a workgroup looks its sequence up among the row blocks of all of them
     int splits;          // parts of the keys, joined by a launch of their own if there are several
     int per_split;       // keys of a part (a multiple of the key tile)
+    int64_t sets;        // key sets that row blocks read: key heads, sequences (unless packed), parts
+    int chunk;           // row blocks of a set that follow one another on an XCD
+    uint32_t grid;
     uint64_t workspace;
 };
 SeqAttnPlan plan_seq_attention(const vpe_attention_args& a);

@@ -33,7 +33,7 @@ __device__ __forceinline__ Seq sequence(const vpe_attention_args& p, int s) {
 
 // What a call's launches share beyond its arguments.
 struct SeqAttnGrid {
-    int blocks, packed, splits, per_split;
+    int blocks, packed, splits, per_split, chunk;
     float *part_o, *part_ml;     // splits > 1: [split][q_rows][heads][D] sums against the part's reference, [split][q_rows][heads][2] (reference, sum)
 };
 
@@ -279,13 +279,18 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
     const int qw = QW > 1 ? wave : 0, kw = KW > 1 ? wave : 0, g = lane >> 5, li = lane & 31;
     const int G = p.heads / p.kv_heads;
 
-    // --- which rows: consecutive workgroups of an XCD have the same keys; the longest row blocks of causal calls come first
-    int lin = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int split = lin % grid.splits;
-    lin /= grid.splits;
-    int blk = lin % grid.blocks, s = 0, kh;
+    // --- which rows.  Runs of `chunk` row blocks that read the same keys (one sequence, key head and part) go to one XCD (consecutive workgroups
+    // to the eight in turn); a run further on every such set has moved to the next XCD, so that long and short sequences spread; and the
+    // longest row blocks of causal calls come first.
+    const int n_sets = p.kv_heads * grid.splits * (grid.packed ? 1 : p.sequences);
+    int t = blockIdx.x >> 3;
+    const int within = t % grid.chunk;
+    t = t / grid.chunk * 8 + (blockIdx.x & 7);
+    const int run = t / n_sets, set = (t + run) % n_sets, split = set % grid.splits, group = set / grid.splits;
+    int blk = run * grid.chunk + within, s = 0, kh;
+    if (blk >= grid.blocks) return;                      // (the grid is whole runs for eight XCDs)
     if (grid.packed) {
-        kh = lin / grid.blocks;
+        kh = group;
         // the sequence that has row block `blk` of all: 64 sequences at a time, a lane counts one's blocks
         int before = 0;
         for (int s0 = 0;; s0 += 64) {
@@ -295,8 +300,8 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
             int sum = n;
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1) {
-                const int t = __shfl_up(sum, o);
-                if (lane >= o) sum += t;
+                const int less = __shfl_up(sum, o);
+                if (lane >= o) sum += less;
             }
             const uint64_t past = __ballot(before + sum > blk);
             if (past) {
@@ -311,9 +316,8 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
         blk = __builtin_amdgcn_readfirstlane(blk);
         if (blk < 0) return;                             // (offsets that make no sense: their counts may have wrapped)
     } else {
-        const int sk = lin / grid.blocks;
-        kh = sk % p.kv_heads;
-        s = sk / p.kv_heads;
+        kh = group % p.kv_heads;
+        s = group / p.kv_heads;
     }
     const Seq sq = sequence(p, s);
     const int64_t rows = (int64_t)sq.nq * G;
@@ -410,7 +414,12 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
 #pragma unroll
             for (int b = 0; b < NB; ++b) sc[b] = M::mma(M::k_frag(tile, 32 * b + li, ks, g), q[ks], sc[b]);
     };
-    auto shape = [&](f32x16 (&sc)[NB], const char* tile, int j0) {      // (not PLAIN) scores in log2 units
+    // c tanh(y / c) / y by the series, x = y^2.  bf16 without the last term (3e-7 of the value)
+    const float c1 = -1.0f / 3.0f * kk, c2 = 2.0f / 15.0f * kk * kk, c3 = -17.0f / 315.0f * kk * kk * kk, c4 = 62.0f / 2835.0f * kk * kk * (kk * kk);
+    auto near_zero = [&](float x) { return fmaf(fmaf(fmaf(sizeof(T) == 4 ? fmaf(c4, x, c3) : c3, x, c2), x, c1), x, 1.0f); };
+    // (not PLAIN) scores in log2 units.  Returns true where the cap is left to the exponentials: all scores are near zero, nothing comes behind
+    // the cap, and so its series goes into their argument
+    auto shape = [&](f32x16 (&sc)[NB], const char* tile, int j0, bool masked) {
         if (p.cap > 0.0f) {
             float top = 0.0f;
 #pragma unroll
@@ -421,14 +430,11 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
                     top = fmaxf(top, fabsf(sc[b][v]));
                 }
             if (series && !__any(top > 0.25f * cap2)) {
-                const float c1 = -1.0f / 3.0f * kk, c2 = 2.0f / 15.0f * kk * kk, c3 = -17.0f / 315.0f * kk * kk * kk, c4 = 62.0f / 2835.0f * kk * kk * (kk * kk);
+                if (MODE == SCORES_LINE && !p.slopes && !masked) return true;
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const float y = sc[b][v], x = y * y;
-                        sc[b][v] = y * fmaf(fmaf(fmaf(fmaf(c4, x, c3), x, c2), x, c1), x, 1.0f);
-                    }
+                    for (int v = 0; v < 16; ++v) sc[b][v] *= near_zero(sc[b][v] * sc[b][v]);
             } else {
                 // c tanh(y / c) = c - 2 c / (1 + e^(2 y / c))
                 const float f = 2.0f * LOG2E / cap2;
@@ -437,11 +443,8 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
                         const float y = sc[b][v], w = fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y * f)), cap2);
-                        if (sizeof(T) == 4) {
-                            const float x = y * y;           // (fp32: near zero the difference above has lost bits)
-                            const float c1 = -1.0f / 3.0f * kk, c2 = 2.0f / 15.0f * kk * kk, c3 = -17.0f / 315.0f * kk * kk * kk, c4 = 62.0f / 2835.0f * kk * kk * (kk * kk);
-                            sc[b][v] = series && fabsf(y) < 0.25f * cap2 ? y * fmaf(fmaf(fmaf(fmaf(c4, x, c3), x, c2), x, c1), x, 1.0f) : w;
-                            if ((v & 3) == 3) __builtin_amdgcn_sched_barrier(0);      // (comparisons of a whole tile at once have no scalar registers)
+                        if (sizeof(T) == 4) {                 // (fp32: near zero the difference above has lost bits)
+                            sc[b][v] = series && fabsf(y) < 0.25f * cap2 ? y * near_zero(y * y) : w;
                         } else {
                             sc[b][v] = w;
                         }
@@ -473,15 +476,20 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
 #pragma unroll
                 for (int v = 0; v < 16; ++v) sc[b][v] = fmaf(-slope2, fabsf(d0 - (float)(32 * b + 8 * (v >> 2) + (v & 3))), sc[b][v]);
         }
+        return false;
     };
     auto compute = [&](const char* stage, int t) {
         const char* tile = stage + kw * OWN;
         const int j0 = j_begin + t * KT;
         if (j0 >= lim_max) return;                        // (the wave's rows see nothing of it)
+        const bool masked = j0 + KT > lim_min || j0 + KT > j_end;
+        bool cap_later = false;
         f32x16 sc[NB];
+        __builtin_amdgcn_s_setprio(1);                    // (of a SIMD's waves the one with products to issue goes first)
         tile_scores(sc, tile);
-        if constexpr (MODE != SCORES_PLAIN) shape(sc, tile, j0);
-        if (j0 + KT > lim_min || j0 + KT > j_end) {
+        __builtin_amdgcn_s_setprio(0);
+        if constexpr (MODE != SCORES_PLAIN) cap_later = shape(sc, tile, j0, masked);
+        if (masked) {
             const int left = (limit < j_end ? limit : j_end) - j0 - 4 * g;
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -496,6 +504,7 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
             for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sc[b][v]);
         mx = halves_max(mx);
         if constexpr (MODE == SCORES_PLAIN) mx *= scale2;
+        if (MODE == SCORES_LINE && cap_later) mx *= near_zero(mx * mx);
         // the reference moves when a row's maximum has grown by more than 8: until then probabilities stay below 2^8, and the wave
         // skips the products with the accumulators
         const bool grow = mx > m + 8.0f;
@@ -508,6 +517,7 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
 #pragma unroll
                 for (int v = 0; v < 16; ++v) o[d][v] *= alpha;
         }
+        __builtin_amdgcn_s_setprio(2);
         const auto values = M::values(tile + TILE, lane);
         auto block = [&](auto ST) {                       // STEPS steps of 16 keys
             Frag f[M::STEPS][DB];
@@ -516,12 +526,21 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
             for (int k = 0; k < M::STEPS; ++k) {
                 constexpr int first = decltype(ST)::value;
                 float e[8];
+                if (MODE == SCORES_LINE && cap_later) {
 #pragma unroll
-                for (int n = 0; n < 8; ++n) {
-                    const float y = sc[(first + k) >> 1][8 * ((first + k) & 1) + n];
-                    e[n] = __builtin_amdgcn_exp2f(MODE == SCORES_PLAIN ? fmaf(y, scale2, -m) : y - m);
-                    l += e[n];
+                    for (int n = 0; n < 8; ++n) {
+                        const float y = sc[(first + k) >> 1][8 * ((first + k) & 1) + n];
+                        e[n] = __builtin_amdgcn_exp2f(fmaf(y, near_zero(y * y), -m));
+                    }
+                } else {
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) {
+                        const float y = sc[(first + k) >> 1][8 * ((first + k) & 1) + n];
+                        e[n] = __builtin_amdgcn_exp2f(MODE == SCORES_PLAIN ? fmaf(y, scale2, -m) : y - m);
+                    }
                 }
+#pragma unroll
+                for (int n = 0; n < 8; ++n) l += e[n];
                 const Frag b = M::probs(e);
 #pragma unroll
                 for (int d = 0; d < DB; ++d) o[d] = M::mma(f[k][d], b, o[d]);
@@ -533,6 +552,7 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
             block(std::integral_constant<int, 2>{});
             if constexpr (M::STEPS == 1) block(std::integral_constant<int, 3>{});
         }
+        __builtin_amdgcn_s_setprio(0);
     };
 
     if constexpr (KW == 1) {
