@@ -10,7 +10,7 @@ namespace vpe {
 
 // Launch plan of an attention call: a function of its sizes alone, so that workspace and grid agree whatever the arrays hold.
 struct SeqAttnPlan {
-    int rows;            // rows of a workgroup: 128 (four waves of 32) or 32 (four waves that share the keys)
+    int rows;            // rows of a workgroup: 128, 64 or 32
     int blocks;          // row blocks of the longest possible sequence, or of all sequences together (`packed`); -1: too many for a launch
     int packed;          // 1: a workgroup looks its sequence up among the row blocks of all of them
     int splits;          // parts of the keys, joined by a launch of their own if there are several

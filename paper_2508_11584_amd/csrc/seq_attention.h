@@ -250,33 +250,34 @@ template <int D> struct SeqMma<float, D> {
     }
 };
 
-// What a score goes through between the two products: nothing but its factor (PLAIN), a cap and distances in a line (LINE), a cap and
-// distances between coordinates (GRID).
-enum { SCORES_PLAIN = 0, SCORES_LINE = 1, SCORES_GRID = 2 };
+// What lowers a score between the two products besides a cap: nothing, distances in a line, distances between coordinates.
+enum { DIST_NONE = 0, DIST_LINE = 1, DIST_GRID = 2 };
 
-template <typename T, int D, int KT, int KW, int MODE>
-constexpr int seq_stage_bytes() { return KW * (2 * KT * SeqMma<T, D>::ROWB + (MODE == SCORES_GRID ? KT * 8 : 0)); }
-template <typename T, int D, int KT, int QW, int KW, int MODE>
+template <typename T, int D, int KT, int KW, int DIST>
+constexpr int seq_stage_bytes() { return KW * (2 * KT * SeqMma<T, D>::ROWB + (DIST == DIST_GRID ? KT * 8 : 0)); }
+template <typename T, int D, int KT, int QW, int KW, int DIST>
 constexpr int seq_lds_bytes() {
-    const int stages = 2 * seq_stage_bytes<T, D, KT, KW, MODE>(), merge = KW > 1 ? KW * 32 * (D + 2) * 4 + 64 : 0;
+    const int stages = 2 * seq_stage_bytes<T, D, KT, KW, DIST>(), merge = KW > 1 ? QW * KW * (32 * (D + 2) * 4 + 4) : 0;
     return stages > merge ? stages : merge;
 }
 
 // A workgroup takes 32 QW consecutive rows of a sequence and key head and the keys of one part; a row is a query and one of the G =
-// heads / kv_heads query heads that read the key head (row r: query r / G, head r % G), so those share every tile.  QW waves of 32 rows
-// share the tiles (KW = 1), or KW waves have all 32 rows and every KW-th tile (QW = 1) and their results meet in LDS, in a fixed order.
+// heads / kv_heads query heads that read the key head (row r: query r / G, head r % G), so those share every tile.  Wave (qw, kw) of QW x KW has 32
+// of the rows and every KW-th tile; a row's KW results meet in LDS and are added in a fixed order.
 // A wave computes scores transposed, S^T = K Q^T: a lane holds half of one row's scores, reductions over the keys stay in the lane but for one
 // exchange, and the probabilities are the second product's operand, O^T = V^T P^T, as they lie.
-template <typename T, int D, int KT, int QW, int KW, int MODE, int OCC>
+// An instantiation per kind of score (with all of them behind run-time branches a tile of slopes alone took 4300 clocks of a lone wave, now XXX; a
+// plain one takes 2100).
+template <typename T, int D, int KT, int QW, int KW, bool CAP, int DIST, int OCC>
 __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const vpe_attention_args p, const SeqAttnGrid grid) {
-    static_assert(QW == 1 || KW == 1, "tiles are shared by all waves or by none");
     using M = SeqMma<T, D>;
     typedef typename M::Frag Frag;
-    constexpr int NW = QW * KW, ROWB = M::ROWB, TILE = KT * ROWB, OWN = 2 * TILE + (MODE == SCORES_GRID ? KT * 8 : 0), STAGE = KW * OWN;
+    constexpr bool PLAIN = !CAP && DIST == DIST_NONE;
+    constexpr int NW = QW * KW, ROWB = M::ROWB, TILE = KT * ROWB, OWN = 2 * TILE + (DIST == DIST_GRID ? KT * 8 : 0), STAGE = KW * OWN;
     constexpr int NB = KT / 32, DB = D / 32, KS = D / 16, CE = Elem<T>::CE;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int qw = QW > 1 ? wave : 0, kw = KW > 1 ? wave : 0, g = lane >> 5, li = lane & 31;
+    const int qw = wave % QW, kw = wave / QW, g = lane >> 5, li = lane & 31;
     const int G = p.heads / p.kv_heads;
 
     // --- which rows.  Runs of `chunk` row blocks that read the same keys (one sequence, key head and part) go to one XCD (consecutive workgroups
@@ -350,15 +351,15 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
     lim_min = __builtin_amdgcn_readfirstlane(lim_min);
     lim_max = __builtin_amdgcn_readfirstlane(lim_max);
 
-    // --- loader: an instruction of a wave fills 1 KB, lane l the 16-byte chunk l of it; the lane fetches the chunk that belongs there
-    constexpr int CPR = ROWB / 16, RPI = 64 / CPR, LW = KW > 1 ? 1 : QW, NI = TILE / 1024 / LW;
+    // --- loader: an instruction of a wave fills 1 KB, lane l the 16-byte chunk l of it; the lane fetches the chunk that belongs there.  QW > 1: call
+    // `t` loads the KW tiles of an iteration, each by all waves; else tile t, by the wave that takes it.
+    constexpr int CPR = ROWB / 16, RPI = 64 / CPR, LW = QW > 1 ? NW : 1, NI = TILE / 1024 / LW;
     static_assert(TILE % (1024 * LW) == 0, "whole instructions");
-    const int lw = KW > 1 ? 0 : wave;
+    const int lw = QW > 1 ? wave : 0;
     const T* kbase = reinterpret_cast<const T*>(p.k) + (int64_t)sq.k0 * p.k_row + kh * p.k_head;
     const T* vbase = reinterpret_cast<const T*>(p.v) + (int64_t)sq.k0 * p.v_row + kh * p.v_head;
-    auto dma = [&](char* stage, int t) {                 // keys j0 .. j0 + KT - 1, those from j_end on as the last of them
+    auto dma_tile = [&](char* own, int t) {              // keys j0 .. j0 + KT - 1, those from j_end on as the last of them
         const int j0 = j_begin + t * KT, last = j_end - 1 - j0;
-        char* own = stage + kw * OWN;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
             const char* base = reinterpret_cast<const char*>((which ? vbase : kbase) + (int64_t)j0 * (which ? p.v_row : p.k_row));
@@ -371,7 +372,7 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
                                                  (__attribute__((address_space(3))) void*)(own + which * TILE + (lw + LW * n) * 1024), 16, 0, 0);
             }
         }
-        if constexpr (MODE == SCORES_GRID) {
+        if constexpr (DIST == DIST_GRID) {
             if (lw == 0) {
 #pragma unroll
                 for (int n = 0; n < KT / 32; ++n) {      // 64 floats = 32 pairs an instruction
@@ -380,6 +381,15 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
                                                      (__attribute__((address_space(3))) void*)(own + 2 * TILE + n * 256), 4, 0, 0);
                 }
             }
+        }
+    };
+    auto dma = [&](char* stage, int t) {
+        if constexpr (QW == 1) {
+            dma_tile(stage + kw * OWN, t);
+        } else {
+#pragma unroll
+            for (int j = 0; j < KW; ++j)
+                if (t * KW + j < tiles) dma_tile(stage + j * OWN, t * KW + j);       // (of the last iteration the tiles that there are)
         }
     };
 
@@ -394,15 +404,29 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int v = 0; v < 16; ++v) o[d][v] = 0.0f;
-    // m: the reference that exponentials are taken against, in log2 units; finite from the start, so that masked scores give zeros
-    float m = -1e30f, l = 0.0f;
+    // m: the reference that exponentials are taken against, in log2 units; `started` when the row has met a key
+    float m = 0.0f, l = 0.0f;
+    bool started = false;
     const float scale2 = p.scale * LOG2E, cap2 = p.cap * LOG2E;
-    const float slope2 = MODE != SCORES_PLAIN && p.slopes ? p.slopes[h] * LOG2E : 0.0f;
+    const float slope2 = DIST != DIST_NONE && p.slopes ? p.slopes[h] * LOG2E : 0.0f;
     f32x2 at = {0.0f, 0.0f};
-    if constexpr (MODE == SCORES_GRID) at = *reinterpret_cast<const f32x2*>(p.q_coords + 2 * row);
-    // tanh(x) for |x| < 1/4 by its series (next term 9e-9 of the value), in x^2 = y^2 / cap2^2 for the score y in log2 units
-    const float kk = MODE != SCORES_PLAIN && p.cap > 0.0f ? 1.0f / (cap2 * cap2) : 0.0f;
+    if constexpr (DIST == DIST_GRID) at = *reinterpret_cast<const f32x2*>(p.q_coords + 2 * row);
+    // c tanh(y / c) = y (1 - x / 3 + 2 x^2 / 15 - 17 x^3 / 315 + 62 x^4 / 2835 - ...), x = (y / c)^2, for scores within c / 4 (what follows is 9e-9 of
+    // the value there; bf16 stops a term earlier, at 3e-7), elsewhere c - 2 c / (1 + e^(2 y / c)), whose difference loses what is near zero
+    const float kk = CAP ? 1.0f / (cap2 * cap2) : 0.0f;
     const bool series = p.cap >= 1e-3f && p.cap <= 1e15f;
+    const float c1 = -1.0f / 3.0f * kk, c2 = 2.0f / 15.0f * kk * kk, c3 = -17.0f / 315.0f * kk * kk * kk, c4 = 62.0f / 2835.0f * kk * kk * (kk * kk);
+    auto near_zero = [&](float y) {
+        const float x = y * y;
+        return fmaf(fmaf(fmaf(sizeof(T) == 4 ? fmaf(c4, x, c3) : c3, x, c2), x, c1), x, 1.0f);
+    };
+    const float tanh_f = CAP ? 2.0f * LOG2E / cap2 * scale2 : 0.0f, near_limit = 0.25f * cap2 / fabsf(scale2);
+    // (of a raw score, less `ref`)
+    auto capped = [&](float s, float ref) { return fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s * tanh_f)), cap2 - ref); };
+    auto capped_near = [&](float s, float ref) {
+        const float y = s * scale2;
+        return fmaf(y, near_zero(y), -ref);
+    };
 
     auto tile_scores = [&](f32x16 (&sc)[NB], const char* tile) {
 #pragma unroll
@@ -413,50 +437,48 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
         for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
             for (int b = 0; b < NB; ++b) sc[b] = M::mma(M::k_frag(tile, 32 * b + li, ks, g), q[ks], sc[b]);
+        if (sizeof(T) == 2) {                             // four fragments are read ahead of their products (7 % of a long causal call)
+            constexpr int AHEAD = 4;
+            __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+            for (int n = 0; n < KS * NB - AHEAD; ++n) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+        }
     };
-    // c tanh(y / c) / y by the series, x = y^2.  bf16 without the last term (3e-7 of the value)
-    const float c1 = -1.0f / 3.0f * kk, c2 = 2.0f / 15.0f * kk * kk, c3 = -17.0f / 315.0f * kk * kk * kk, c4 = 62.0f / 2835.0f * kk * kk * (kk * kk);
-    auto near_zero = [&](float x) { return fmaf(fmaf(fmaf(sizeof(T) == 4 ? fmaf(c4, x, c3) : c3, x, c2), x, c1), x, 1.0f); };
-    // (not PLAIN) scores in log2 units.  Returns true where the cap is left to the exponentials: all scores are near zero, nothing comes behind
-    // the cap, and so its series goes into their argument
-    auto shape = [&](f32x16 (&sc)[NB], const char* tile, int j0, bool masked) {
-        if (p.cap > 0.0f) {
-            float top = 0.0f;
+    // Is every score of the tile near zero, as caps go?
+    auto all_near = [&](const f32x16 (&sc)[NB]) {
+        float top = 0.0f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) top = fmaxf(top, fabsf(sc[b][v]));
+        return series && !__any(top > near_limit);
+    };
+    // Makes raw scores exponents: in log2 units, capped, lowered by distance, less the reference.
+    auto shape = [&](f32x16 (&sc)[NB], const char* tile, int j0) {
+        if constexpr (!CAP) {
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    sc[b][v] *= scale2;
-                    top = fmaxf(top, fabsf(sc[b][v]));
-                }
-            if (series && !__any(top > 0.25f * cap2)) {
-                if (MODE == SCORES_LINE && !p.slopes && !masked) return true;
+                for (int v = 0; v < 16; ++v) sc[b][v] = fmaf(sc[b][v], scale2, -m);
+        } else if (all_near(sc)) {
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) sc[b][v] *= near_zero(sc[b][v] * sc[b][v]);
-            } else {
-                // c tanh(y / c) = c - 2 c / (1 + e^(2 y / c))
-                const float f = 2.0f * LOG2E / cap2;
-#pragma unroll
-                for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const float y = sc[b][v], w = fmaf(-2.0f * cap2, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y * f)), cap2);
-                        if (sizeof(T) == 4) {                 // (fp32: near zero the difference above has lost bits)
-                            sc[b][v] = series && fabsf(y) < 0.25f * cap2 ? y * near_zero(y * y) : w;
-                        } else {
-                            sc[b][v] = w;
-                        }
-                    }
-            }
+                for (int v = 0; v < 16; ++v) sc[b][v] = capped_near(sc[b][v], m);
         } else {
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) sc[b][v] *= scale2;
+                for (int v = 0; v < 16; ++v) {
+                    const float s = sc[b][v];
+                    sc[b][v] = sizeof(T) == 4 && series && fabsf(s) < near_limit ? capped_near(s, m) : capped(s, m);
+                }
         }
-        if constexpr (MODE == SCORES_GRID) {
+        if constexpr (DIST == DIST_GRID) {
             const char* c = tile + 2 * TILE + 32 * g;
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -469,26 +491,78 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
                         sc[b][2 * n + e] = fmaf(-slope2, __builtin_amdgcn_sqrtf(fmaf(dy, dy, dx * dx)), sc[b][2 * n + e]);
                     }
                 }
-        } else if (p.slopes) {
+        } else if constexpr (DIST == DIST_LINE) {
             const float d0 = (float)(place - j0 - 4 * g);
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) sc[b][v] = fmaf(-slope2, fabsf(d0 - (float)(32 * b + 8 * (v >> 2) + (v & 3))), sc[b][v]);
         }
-        return false;
+    };
+    // (plain scores stay raw: their factor and the reference are part of the exponentials' argument)
+    auto exponent = [&](float s) { return PLAIN ? fmaf(s, scale2, -m) : s; };
+    auto finish = [&](f32x16 (&sc)[NB], const char* tile) {
+        float rel = sc[0][0];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) rel = fmaxf(rel, sc[b][v]);
+        rel = exponent(halves_max(rel));
+        // the reference moves with a row's first key and when its maximum has grown by more than 8: until then probabilities stay below 2^8,
+        // and the wave skips the products with the accumulators
+        const bool grow = rel > 8.0f || (!started && rel > -INFINITY);
+        if (__any(grow)) {
+            const float by = grow ? rel : 0.0f, alpha = started ? __builtin_amdgcn_exp2f(-by) : 1.0f;
+            m += by;
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) o[d][v] *= alpha;
+            if constexpr (!PLAIN) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) sc[b][v] -= by;
+            }
+        }
+        started = started || rel > -INFINITY;
+        __builtin_amdgcn_s_setprio(2);
+        const auto values = M::values(tile + TILE, lane);
+        auto block = [&](auto N) {                        // STEPS steps of 16 keys
+            constexpr int first = decltype(N)::value * M::STEPS;
+            Frag f[M::STEPS][DB];
+            M::template v_frags<first>(values, f);
+#pragma unroll
+            for (int k = 0; k < M::STEPS; ++k) {
+                float e[8];
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    e[n] = __builtin_amdgcn_exp2f(exponent(sc[(first + k) >> 1][8 * ((first + k) & 1) + n]));
+                    l += e[n];
+                }
+                const Frag b = M::probs(e);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) o[d] = M::mma(f[k][d], b, o[d]);
+            }
+        };
+        constexpr int BLOCKS = KT / 16 / M::STEPS;
+        block(std::integral_constant<int, 0>{});
+        if constexpr (BLOCKS > 1) block(std::integral_constant<int, 1>{});
+        if constexpr (BLOCKS > 2) block(std::integral_constant<int, 2>{});
+        if constexpr (BLOCKS > 3) block(std::integral_constant<int, 3>{});
+        __builtin_amdgcn_s_setprio(0);
     };
     auto compute = [&](const char* stage, int t) {
         const char* tile = stage + kw * OWN;
         const int j0 = j_begin + t * KT;
         if (j0 >= lim_max) return;                        // (the wave's rows see nothing of it)
         const bool masked = j0 + KT > lim_min || j0 + KT > j_end;
-        bool cap_later = false;
         f32x16 sc[NB];
         __builtin_amdgcn_s_setprio(1);                    // (of a SIMD's waves the one with products to issue goes first)
         tile_scores(sc, tile);
         __builtin_amdgcn_s_setprio(0);
-        if constexpr (MODE != SCORES_PLAIN) cap_later = shape(sc, tile, j0, masked);
+        if constexpr (!PLAIN) shape(sc, tile, j0);
         if (masked) {
             const int left = (limit < j_end ? limit : j_end) - j0 - 4 * g;
 #pragma unroll
@@ -497,71 +571,18 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
                 for (int v = 0; v < 16; ++v)
                     if (32 * b + 8 * (v >> 2) + (v & 3) >= left) sc[b][v] = -INFINITY;
         }
-        float mx = sc[0][0];
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sc[b][v]);
-        mx = halves_max(mx);
-        if constexpr (MODE == SCORES_PLAIN) mx *= scale2;
-        if (MODE == SCORES_LINE && cap_later) mx *= near_zero(mx * mx);
-        // the reference moves when a row's maximum has grown by more than 8: until then probabilities stay below 2^8, and the wave
-        // skips the products with the accumulators
-        const bool grow = mx > m + 8.0f;
-        if (__any(grow)) {
-            const float top = grow ? mx : m, alpha = __builtin_amdgcn_exp2f(m - top);
-            m = top;
-            l *= alpha;
-#pragma unroll
-            for (int d = 0; d < DB; ++d)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) o[d][v] *= alpha;
-        }
-        __builtin_amdgcn_s_setprio(2);
-        const auto values = M::values(tile + TILE, lane);
-        auto block = [&](auto ST) {                       // STEPS steps of 16 keys
-            Frag f[M::STEPS][DB];
-            M::template v_frags<decltype(ST)::value>(values, f);
-#pragma unroll
-            for (int k = 0; k < M::STEPS; ++k) {
-                constexpr int first = decltype(ST)::value;
-                float e[8];
-                if (MODE == SCORES_LINE && cap_later) {
-#pragma unroll
-                    for (int n = 0; n < 8; ++n) {
-                        const float y = sc[(first + k) >> 1][8 * ((first + k) & 1) + n];
-                        e[n] = __builtin_amdgcn_exp2f(fmaf(y, near_zero(y * y), -m));
-                    }
-                } else {
-#pragma unroll
-                    for (int n = 0; n < 8; ++n) {
-                        const float y = sc[(first + k) >> 1][8 * ((first + k) & 1) + n];
-                        e[n] = __builtin_amdgcn_exp2f(MODE == SCORES_PLAIN ? fmaf(y, scale2, -m) : y - m);
-                    }
-                }
-#pragma unroll
-                for (int n = 0; n < 8; ++n) l += e[n];
-                const Frag b = M::probs(e);
-#pragma unroll
-                for (int d = 0; d < DB; ++d) o[d] = M::mma(f[k][d], b, o[d]);
-            }
-        };
-        block(std::integral_constant<int, 0>{});
-        if constexpr (M::STEPS == 1) block(std::integral_constant<int, 1>{});
-        if constexpr (KT == 64) {
-            block(std::integral_constant<int, 2>{});
-            if constexpr (M::STEPS == 1) block(std::integral_constant<int, 3>{});
-        }
-        __builtin_amdgcn_s_setprio(0);
+        finish(sc, tile);
     };
 
-    if constexpr (KW == 1) {
-        if (tiles > 0) dma(smem, 0);
+    if constexpr (QW > 1) {
+        // all waves load all tiles of an iteration (KW of them), and wait for each other
+        const int turns = (tiles + KW - 1) / KW;
+        if (turns > 0) dma(smem, 0);
         __builtin_amdgcn_s_waitcnt(0x0F70);               // vmcnt(0): the loads into LDS have landed
         __syncthreads();
-        for (int t = 0; t < tiles; ++t) {
-            if (t + 1 < tiles) dma(smem + ((t + 1) & 1) * STAGE, t + 1);
-            compute(smem + (t & 1) * STAGE, t);
+        for (int it = 0; it < turns; ++it) {
+            if (it + 1 < turns) dma(smem + ((it + 1) & 1) * STAGE, it + 1);
+            if (KW == 1 || it * KW + kw < tiles) compute(smem + (it & 1) * STAGE, it * KW + kw);
             __builtin_amdgcn_s_waitcnt(0x0F70);
             __syncthreads();
         }
@@ -573,7 +594,7 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
             if (t + KW < tiles) {
                 dma(smem + (buf ^ 1) * STAGE, t + KW);
                 __builtin_amdgcn_sched_barrier(0);
-                __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * NI + (MODE == SCORES_GRID ? KT / 32 : 0)));
+                __builtin_amdgcn_s_waitcnt(vmcnt_imm(2 * NI + (DIST == DIST_GRID ? KT / 32 : 0)));
             } else {
                 __builtin_amdgcn_s_waitcnt(0x0F70);
             }
@@ -584,6 +605,7 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
         }
         __syncthreads();
     }
+    if (!started) m = -1e30f;
     l = halves_sum(l);
 
     // --- results.  A row is handed to attention_row if a sum of it is not finite, or nothing if it sees keys.  (The arguments are read once
@@ -619,65 +641,65 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
             attention_row<T, D>(p, grid, sq, ii, kh * G + (int)(rr - (int64_t)ii * G), j_begin, j_stop, split, lane);
         }
     } else {
-        // every wave leaves its sums, (c, row) 16 bytes apart by row, and its (m, l); then a thread adds four columns of a row
+        // every wave leaves its sums, (c, row) 16 bytes apart by row, and its (m, l); then a thread of a row's KW waves adds four columns
         constexpr int RED = 32 * D;                       // floats of a wave's sums
         float* sums = reinterpret_cast<float*>(smem);
-        float* ml = sums + KW * RED;
+        float* ml = sums + NW * RED;
         __syncthreads();
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int n = 0; n < 4; ++n)
-                *reinterpret_cast<f32x4*>(sums + kw * RED + ((8 * d + 2 * n + g) * 32 + li) * 4) = f32x4{o[d][4 * n], o[d][4 * n + 1], o[d][4 * n + 2], o[d][4 * n + 3]};
-        if (g == 0) *reinterpret_cast<f32x2*>(ml + (kw * 32 + li) * 2) = f32x2{m, l};
+                *reinterpret_cast<f32x4*>(sums + wave * RED + ((8 * d + 2 * n + g) * 32 + li) * 4) = f32x4{o[d][4 * n], o[d][4 * n + 1], o[d][4 * n + 2], o[d][4 * n + 3]};
+        if (g == 0) *reinterpret_cast<f32x2*>(ml + (wave * 32 + li) * 2) = f32x2{m, l};
         __syncthreads();
         float w[KW], top = -1e30f, total = 0.0f;
 #pragma unroll
-        for (int k = 0; k < KW; ++k) top = fmaxf(top, ml[(k * 32 + li) * 2]);
+        for (int k = 0; k < KW; ++k) top = fmaxf(top, ml[((k * QW + qw) * 32 + li) * 2]);
 #pragma unroll
         for (int k = 0; k < KW; ++k) {
-            w[k] = __builtin_amdgcn_exp2f(ml[(k * 32 + li) * 2] - top);
-            total += w[k] * ml[(k * 32 + li) * 2 + 1];
+            w[k] = __builtin_amdgcn_exp2f(ml[((k * QW + qw) * 32 + li) * 2] - top);
+            total += w[k] * ml[((k * QW + qw) * 32 + li) * 2 + 1];
         }
         const float f = grid.splits > 1 || total == 0.0f ? 1.0f : 1.0f / total;
         float odd = total * 0.0f;
-        constexpr int PER = D / 4 / (2 * NW);             // column groups of a thread
+        constexpr int PER = D / 4 / (2 * KW);             // column groups of a thread
         f32x4 out[PER];
 #pragma unroll
         for (int n = 0; n < PER; ++n) {
-            const int c = (2 * wave + g) + 2 * NW * n;
+            const int c = (2 * kw + g) + 2 * KW * n;
             out[n] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int k = 0; k < KW; ++k) {
-                const f32x4 v = *reinterpret_cast<const f32x4*>(sums + k * RED + (c * 32 + li) * 4);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(sums + (k * QW + qw) * RED + (c * 32 + li) * 4);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) out[n][e] = fmaf(w[k], v[e], out[n][e]);
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) odd = fmaf(out[n][e], 0.0f, odd);
         }
-        // a bad row is bad for all waves: they tell each other before anybody stores
-        uint32_t* flags = reinterpret_cast<uint32_t*>(ml + KW * 64);
+        // a row that is bad for one of its waves is for all: they tell each other before anybody stores
+        uint32_t* flags = reinterpret_cast<uint32_t*>(ml + NW * 64);
         uint64_t mine = __ballot(real && (odd != odd || (total == 0.0f && seen_end > j_begin)));
         if (lane == 0) flags[wave] = (uint32_t)(mine | mine >> 32);
         __syncthreads();
         uint32_t redo = 0;
 #pragma unroll
-        for (int k = 0; k < NW; ++k) redo |= flags[k];
+        for (int k = 0; k < KW; ++k) redo |= flags[k * QW + qw];
         if (real && !((redo >> li) & 1)) {
 #pragma unroll
             for (int n = 0; n < PER; ++n) {
-                const int c = ((2 * wave + g) + 2 * NW * n) * 4;
+                const int c = ((2 * kw + g) + 2 * KW * n) * 4;
                 const float v[4] = {out[n][0] * f, out[n][1] * f, out[n][2] * f, out[n][3] * f};
                 if (grid.splits > 1) store_columns<4>(grid.part_o + part_row(p, row, h, split) * D + c, v);
                 else store_columns<4>(reinterpret_cast<T*>(p.out) + row * p.out_row + h * p.out_head + c, v);
             }
-            if (wave == 0 && g == 0) store_stats<T>(p, grid, row, h, split, top, total);
+            if (kw == 0 && g == 0) store_stats<T>(p, grid, row, h, split, top, total);
         }
         int n = 0;
         for (uint32_t left = __builtin_amdgcn_readfirstlane(redo); left; left &= left - 1, ++n) {
-            if (n % NW != wave) continue;
-            const int64_t rr = r0 + __builtin_ctz(left);
+            if (n % KW != kw) continue;
+            const int64_t rr = r0 + qw * 32 + __builtin_ctz(left);
             const int ii = (int)(rr / G);
             attention_row<T, D>(p, grid, sq, ii, kh * G + (int)(rr - (int64_t)ii * G), j_begin, j_stop, split, lane);
         }
@@ -706,24 +728,42 @@ __global__ __launch_bounds__(256) void seq_attention_join_kernel(const vpe_atten
         found = __any(in);
     }
     if (!found) return;
+    // a lane has a part's reference and sum (up to 64 parts), then one or two columns of all parts, several loads on their way
     constexpr int ND = D / 64;
-    float m = -INFINITY, l = 0.0f, acc[ND];
+    f32x2 ml = {-INFINITY, 0.0f};
+    if (lane < grid.splits) ml = *reinterpret_cast<const f32x2*>(grid.part_ml + 2 * part_row(p, row, h, lane));
+    float m = ml[1] == 0.0f ? -INFINITY : ml[0];          // (no keys of the row in this part)
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    const float w = ml[1] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ml[0] - m);
+    const float l = wave_sum(ml[1] == 0.0f ? 0.0f : ml[1] * w);
+    float acc[ND];
 #pragma unroll
     for (int n = 0; n < ND; ++n) acc[n] = 0.0f;
+    const float* part = grid.part_o + part_row(p, row, h, 0) * D + lane;
+    const int64_t step = n_rows * D;
+#pragma unroll 8
     for (int k = 0; k < grid.splits; ++k) {
-        const int64_t at = part_row(p, row, h, k);
-        const f32x2 ml = *reinterpret_cast<const f32x2*>(grid.part_ml + 2 * at);
-        if (ml[1] == 0.0f) continue;                      // (nothing of the row in this part)
-        const float top = fmaxf(m, ml[0]), a = __builtin_amdgcn_exp2f(m - top), b = __builtin_amdgcn_exp2f(ml[0] - top);
-        l = l * a + ml[1] * b;
-        m = top;
+        const float by = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), k));
 #pragma unroll
-        for (int n = 0; n < ND; ++n) acc[n] = acc[n] * a + grid.part_o[at * D + 64 * n + lane] * b;
+        for (int n = 0; n < ND; ++n) {
+            const float v = part[k * step + 64 * n];
+            acc[n] += by == 0.0f ? 0.0f : by * v;
+        }
     }
 #pragma unroll
     for (int n = 0; n < ND; ++n)
         reinterpret_cast<T*>(p.out)[row * p.out_row + h * p.out_head + 64 * n + lane] = from_f32<T>(l == 0.0f ? 0.0f : acc[n] / l);
     if (p.lse && lane == 0) p.lse[row * p.heads + h] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
 }
+
+// What a launch needs to know of an instantiation.
+typedef void (*SeqKernel)(const vpe_attention_args, const SeqAttnGrid);
+struct SeqShape { SeqKernel kernel; int threads, lds; };
+template <typename T, int D, int KT, int QW, int KW, bool CAP, int DIST, int OCC>
+SeqShape seq_shape() { return {&seq_attention_kernel<T, D, KT, QW, KW, CAP, DIST, OCC>, 64 * QW * KW, seq_lds_bytes<T, D, KT, QW, KW, DIST>()}; }
+// The instantiation for a kind of score, a head's width and a workgroup's rows (a translation unit per type).
+SeqShape seq_shape_bf16(bool cap, int dist, int head_dim, int rows);
+SeqShape seq_shape_f32(bool cap, int dist, int head_dim, int rows);
 
 }  // namespace vpe

@@ -1,6 +1,5 @@
 // Instantiations, plan and launch of the attention over packed sequences.
 #include <algorithm>
-#include <cstdlib>
 
 #include "operators.h"
 #include "seq_attention.h"
@@ -8,29 +7,12 @@
 namespace vpe {
 namespace {
 
-typedef void (*Kernel)(const vpe_attention_args, const SeqAttnGrid);
-// What a launch needs to know of a shape: rows of a workgroup, threads, LDS, keys that it takes at a time.
-struct Shape { Kernel kernel; int rows, threads, lds, keys; };
-
-template <typename T, int D, int KT, int QW, int KW, int MODE, int OCC>
-Shape shape() { return {&seq_attention_kernel<T, D, KT, QW, KW, MODE, OCC>, 32 * QW, 64 * QW * KW, seq_lds_bytes<T, D, KT, QW, KW, MODE>(), KT * KW}; }
-
-template <int MODE>
-Shape shape_of(int dtype, int head_dim, int rows) {
-    // (with coordinates 64 keys of fp32 at a time take a register too many)
-    constexpr int F64 = MODE == SCORES_GRID ? 32 : 64;
-    if (dtype == VPE_BF16) {
-        if (head_dim == 64) return rows == 128 ? shape<bf16, 64, 64, 4, 1, MODE, 3>() : shape<bf16, 64, 32, 1, 4, MODE, 2>();
-        return rows == 128 ? shape<bf16, 128, 64, 4, 1, MODE, 2>() : shape<bf16, 128, 32, 1, 4, MODE, 1>();
-    }
-    if (head_dim == 64) return rows == 128 ? shape<float, 64, F64, 4, 1, MODE, 2>() : shape<float, 64, 32, 1, 4, MODE, 1>();
-    return rows == 128 ? shape<float, 128, 32, 4, 1, MODE, 1>() : shape<float, 128, 32, 1, 2, MODE, 1>();
-}
-Shape shape_of(const vpe_attention_args& a, const SeqAttnPlan& plan) {
-    // (a factor that is not positive turns maxima of raw scores round, a tiny one could make 0 x infinity of masked ones: LINE multiplies first)
-    if (a.q_coords) return shape_of<SCORES_GRID>(a.dtype, a.head_dim, plan.rows);
-    if (a.cap > 0.0f || a.slopes || !(a.scale > 1e-30f)) return shape_of<SCORES_LINE>(a.dtype, a.head_dim, plan.rows);
-    return shape_of<SCORES_PLAIN>(a.dtype, a.head_dim, plan.rows);
+SeqShape shape_of(const vpe_attention_args& a, const SeqAttnPlan& plan) {
+    // (plain scores stay raw until the exponential: a factor that is not positive would turn their order round, a tiny one make 0 x infinity of
+    // hidden ones; LINE multiplies first, and without slopes takes nothing off)
+    const bool cap = a.cap > 0.0f;
+    const int dist = a.q_coords ? DIST_GRID : a.slopes || (!cap && !(a.scale > 1e-30f)) ? DIST_LINE : DIST_NONE;
+    return a.dtype == VPE_BF16 ? seq_shape_bf16(cap, dist, a.head_dim, plan.rows) : seq_shape_f32(cap, dist, a.head_dim, plan.rows);
 }
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -48,16 +30,20 @@ SeqAttnPlan plan_seq_attention(const vpe_attention_args& a) {
         plan.sets = a.kv_heads * (int64_t)(plan.packed ? 1 : a.sequences);
         return plan.packed ? all : direct;
     };
-    int64_t blocks = most > 32 ? with_rows(128) : 0;
-    const int th = getenv("SA_TH") ? atoi(getenv("SA_TH")) : 384, tg = getenv("SA_TG") ? atoi(getenv("SA_TG")) : 512;
-    if (most <= 32 || blocks * plan.sets < (getenv("SA_W") ? atoi(getenv("SA_W")) : 384)) blocks = with_rows(32);
+    // us, workgroups of 128 rows (four waves of 32) / 64 (two, by two that share the keys) / 32 (four that share the keys), by workgroups of 128:
+    //     72  ViT-S 476x630         26 / 22 / 15       176  ViT-L 518x518             34 / 25 / 27.5    2112  ViT-g 518x518 x 8           130 / 160 / 219
+    //    132  ViT-B 518x518         30 / 24 / 26       264  ViT-B 518x518 x 2         32 / 31 / 38       256  8192 causal, 16 heads of 128  292 / 359 / 665
+    //    132  the same, a grid      36 / 35 / 33       352  ViT-L 518x518 x 2         33 / 32 / 42       410  five views on a grid         60 / 60 / 64
+    //    132  the same, fp32        68 / 75 / 90       192  3000 fp32, 8 heads of 128 190 / 187 / 304
+    // Few rows: one launch is as long as its longest workgroup, so the keys are shared by more waves; many: reading the tiles counts, and a
+    // workgroup's rows share them.  fp32 waves split every operand that they read: keys shared by four waves of 32 rows are split four times as often.
+    int64_t blocks = with_rows(most <= 32 ? 32 : 128);
+    if (most > 32 && blocks * plan.sets < 256) blocks = with_rows(a.dtype == VPE_F32 || blocks * plan.sets >= 96 ? 64 : 32);
+    // Parts of at least 256 keys until two workgroups for every CU are there
     const int64_t base = blocks * plan.sets;
-    plan.splits = 1;
-    const int keys = 256;
-    if (base < th) plan.splits = (int)std::min<int64_t>({tg / base, up(a.max_k, keys), 64});
-    if (plan.splits < 1) plan.splits = 1;
+    plan.splits = base < 256 ? (int)std::max<int64_t>(1, std::min<int64_t>({512 / base, up(a.max_k, 256), 64})) : 1;
     plan.per_split = (int)up(up(a.max_k, plan.splits), 128) * 128;
-    if (plan.per_split < 128) plan.per_split = 128;
+    plan.per_split = std::max(plan.per_split, 128);
     plan.splits = (int)std::max<int64_t>(1, up(a.max_k, plan.per_split));
     plan.sets *= plan.splits;
     plan.chunk = (int)std::max<int64_t>(1, std::min<int64_t>({16, blocks, blocks * plan.sets / 64}));
@@ -70,7 +56,7 @@ SeqAttnPlan plan_seq_attention(const vpe_attention_args& a) {
 }
 
 hipError_t launch_seq_attention(const vpe_attention_args& a, const SeqAttnPlan& plan, hipStream_t s) {
-    const Shape k = shape_of(a, plan);
+    const SeqShape k = shape_of(a, plan);
     SeqAttnGrid grid{plan.blocks, plan.packed, plan.splits, plan.per_split, plan.chunk, nullptr, nullptr};
     if (plan.splits > 1) {
         grid.part_o = reinterpret_cast<float*>(a.workspace);
@@ -83,7 +69,7 @@ hipError_t launch_seq_attention(const vpe_attention_args& a, const SeqAttnPlan& 
     hipLaunchKernelGGL(k.kernel, dim3(plan.grid), dim3(k.threads), k.lds, s, a, grid);
     hipError_t rc = hipGetLastError();
     if (rc != hipSuccess || plan.splits == 1) return rc;
-    const Kernel join = a.dtype == VPE_BF16 ? (a.head_dim == 64 ? &seq_attention_join_kernel<bf16, 64> : &seq_attention_join_kernel<bf16, 128>)
+    const SeqKernel join = a.dtype == VPE_BF16 ? (a.head_dim == 64 ? &seq_attention_join_kernel<bf16, 64> : &seq_attention_join_kernel<bf16, 128>)
                                             : (a.head_dim == 64 ? &seq_attention_join_kernel<float, 64> : &seq_attention_join_kernel<float, 128>);
     hipLaunchKernelGGL(join, dim3((uint32_t)up((int64_t)a.q_rows * a.heads, 4)), dim3(256), 0, s, a, grid);
     return hipGetLastError();
