@@ -8,13 +8,21 @@
 
 #include "kernels.h"
 #include "operators.h"
+#include "wave_sum.h"
 
 namespace vpe {
 namespace {
 
 int rank16(const vpe_adapter_linear_args& a) { return (a.rank + 15) / 16 * 16; }
-// Rows up to which the projection is bound by its weight and read by many workgroups (skinny_kernel); more go to the tiled GEMM.
-constexpr int SKINNY_ROWS = 64;
+// Rows up to which the projection goes to skinny_kernel, which reads the weight once with workgroups of 16 columns; beyond, x, read by every
+// one of them, is most of what they load, and the tiled GEMM shares it among 64 columns.  us, skinny / tiled, bf16 and fp32, rank 16, 1536 x
+// 4608 and 4096 x 4096: 17 rows 14.2 / 14.1, 26 / 45; 32 rows 16.0 / 14.1, 24.5 / 30.6; 48 rows 20.2 / 13.0, 34 / 29 and 23.1 / 22.8, 42.7 / 49.7;
+// 64 rows 25 / 11.6, 43 / 26.4 and 27 / 22, 59 / 48.
+template <typename T> constexpr int skinny_rows() { return sizeof(T) == 2 ? 16 : 32; }
+// Rows up to which a wave makes one low-rank value (us a call, such waves / those of 4 x 8 values: 512 rows of 1536 20.7 / 25.7, 1000 33 / 37.5,
+// 4000 86 / 78, of mixed adapters 112 / 110; 10992 rows, rank 32 275 / 218).
+constexpr int ONE_VALUE_ROWS = 1024;
+constexpr int WAVES = 8;            // of a workgroup that shares a width
 
 template <typename T> __device__ __forceinline__ void unpack(const u32x4& raw, float* v) {
     T e[Elem<T>::CE];
@@ -37,96 +45,89 @@ __device__ __forceinline__ void leave(void* t, int64_t row, int ld, int j, int h
     }
 }
 
-// t of few rows: a wave per row and rank index, 16 bytes a lane.  Whatever adapters the rows have, each adapter row is read once per row.
-template <typename T, bool TERMS>
-__global__ __launch_bounds__(256) void adapter_rows_kernel(const vpe_adapter_linear_args p, void* t, int r16) {
-    const int lane = threadIdx.x & 63;
-    const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), row = task / r16;
-    const int j = (int)(task - row * r16);
-    if (row >= p.rows) return;
-    const int a = p.adapter[row], ld = TERMS && sizeof(T) == 2 ? 2 * r16 : r16;
-    if (a < 0 || a >= p.adapters) return;                     // (its t is not looked at)
-    float sum = 0.0f;
-    if (j < p.rank) {
-        constexpr int CE = Elem<T>::CE;
-        const T* x = reinterpret_cast<const T*>(p.x) + row * p.x_row;
-        const T* w = reinterpret_cast<const T*>(p.a) + ((int64_t)a * p.rank + j) * p.in_features;
-        for (int k = lane * CE; k < p.in_features; k += 64 * CE) {
-            float u[CE], v[CE];
-            unpack<T>(ld_global_16(x + k), u);
-            unpack<T>(ld_global_16(w + k), v);
+// Sum of eight (four) products of 16 bytes of two rows, added to `sum` in fp32.
+template <typename T> __device__ __forceinline__ float dot16(const u32x4& a, const u32x4& b, float sum) {
+    if constexpr (sizeof(T) == 2) {
+        // (two exact products and their sum an instruction: no conversions)
 #pragma unroll
-            for (int i = 0; i < CE; ++i) sum = fmaf(u[i], v[i], sum);
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t u = a[i], v = b[i];                // (a cast of the element itself takes the first)
+            sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, u), __builtin_bit_cast(bf16x2, v), sum, false);
         }
-        sum = wave_sum(sum);
-        if (p.scale) sum *= p.scale[a];
+    } else {
+        const f32x4 u = __builtin_bit_cast(f32x4, a), v = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum = fmaf(u[i], v[i], sum);
     }
-    if (lane == 0) leave<T, TERMS>(t, row, ld, j, r16, sum);
+    return sum;
 }
 
-// t of many rows: 32 rows a workgroup, their width shared by eight waves, 32 rank indices at a time, once for every adapter among the rows.
-// Bound by reading x where rows of an adapter lie together.
-template <typename T>
-__global__ __launch_bounds__(512) void adapter_tiles_kernel(const vpe_adapter_linear_args p, void* t, int r16) {
-    __shared__ __attribute__((aligned(16))) float part[8][32 * 32];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 5, li = lane & 31, ld = sizeof(T) == 2 ? 2 * r16 : r16;
-    const int row0 = blockIdx.x * 32, r = row0 + li < p.rows ? row0 + li : p.rows - 1;
-    const int id = p.adapter[r], per = cdiv(p.in_features / 16, 8), k0 = wave * per * 16, k1 = k0 + per * 16 < p.in_features ? k0 + per * 16 : p.in_features;
-    const T* x = reinterpret_cast<const T*>(p.x) + (int64_t)r * p.x_row + 8 * g;
-    for (uint64_t todo = __ballot(id >= 0 && id < p.adapters); todo;) {
-        const int a = __builtin_amdgcn_readlane(id, __builtin_ctzll(todo));
-        const uint64_t rows = __ballot(id == a);
-        todo &= ~rows;
+// t: a wave has R rows and J rank indices, 16 bytes of each a lane at a time, once for every adapter among its rows.  One of each for few rows:
+// as many waves as there are values, and an adapter is read for the rows that have it; four rows and eight indices for many: twelve
+// loads make thirty-two values where one of each makes one of two.
+template <typename T, bool TERMS, int R, int J>
+__global__ __launch_bounds__(256) void adapter_down_kernel(const vpe_adapter_linear_args p, void* t, int r16) {
+    constexpr int CE = Elem<T>::CE;
+    const int lane = threadIdx.x & 63, ld = TERMS && sizeof(T) == 2 ? 2 * r16 : r16, per_row = r16 / J;
+    const int64_t task = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = task / per_row * R;
+    const int j0 = (int)(task % per_row) * J;
+    if (row0 >= p.rows) return;
+    const T* x[R];
+    int id[R];
+#pragma unroll
+    for (int n = 0; n < R; ++n) {
+        const int64_t r = row0 + n < p.rows ? row0 + n : p.rows - 1;
+        x[n] = reinterpret_cast<const T*>(p.x) + r * p.x_row;
+        id[n] = row0 + n < p.rows ? __builtin_amdgcn_readfirstlane(p.adapter[r]) : -1;
+    }
+#pragma unroll
+    for (int first = 0; first < R; ++first) {
+        const int a = id[first];
+        if (a < 0 || a >= p.adapters) continue;               // (its t is not looked at)
+        bool done = false;
+#pragma unroll
+        for (int n = 0; n < first; ++n) done = done || id[n] == a;
+        if (done) continue;
+        const T* w[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) w[j] = reinterpret_cast<const T*>(p.a) + ((int64_t)a * p.rank + (j0 + j < p.rank ? j0 + j : p.rank - 1)) * p.in_features;
+        float sum[R][J];
+#pragma unroll
+        for (int n = 0; n < R; ++n)
+#pragma unroll
+            for (int j = 0; j < J; ++j) sum[n][j] = 0.0f;
+        for (int k = lane * CE; k < p.in_features; k += 64 * CE) {
+            u32x4 xv[R], wv[J];
+#pragma unroll
+            for (int n = 0; n < R; ++n) xv[n] = ld_global_16(x[n] + k);
+#pragma unroll
+            for (int j = 0; j < J; ++j) wv[j] = ld_global_16(w[j] + k);
+#pragma unroll
+            for (int n = 0; n < R; ++n)
+#pragma unroll
+                for (int j = 0; j < J; ++j) sum[n][j] = dot16<T>(xv[n], wv[j], sum[n][j]);
+        }
         const float scale = p.scale ? p.scale[a] : 1.0f;
-        for (int j0 = 0; j0 < r16; j0 += 32) {
-            const int j = j0 + li < p.rank ? j0 + li : p.rank - 1;
-            const T* w = reinterpret_cast<const T*>(p.a) + ((int64_t)a * p.rank + j) * p.in_features + 8 * g;
-            f32x16 c;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) c[v] = 0.0f;
-#pragma unroll 4
-            for (int k = k0; k < k1; k += 16) {
-                if constexpr (sizeof(T) == 2) {
-                    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(w + k), *reinterpret_cast<const bf16x8*>(x + k), c, 0, 0, 0);
-                } else {
-                    const f32x4 w0 = *reinterpret_cast<const f32x4*>(w + k), w1 = *reinterpret_cast<const f32x4*>(w + k + 4);
-                    const f32x4 x0 = *reinterpret_cast<const f32x4*>(x + k), x1 = *reinterpret_cast<const f32x4*>(x + k + 4);
+        for (int n = 0; n < R; ++n) {
+            if (id[n] != a) continue;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(w0[e], x0[e], c, 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(w1[e], x1[e], c, 0, 0, 0);
-                }
+            for (int j = 0; j < J; ++j) {
+                const float v = wave_total(sum[n][j]);
+                if (lane == 0) leave<T, TERMS>(t, row0 + n, ld, j0 + j, r16, j0 + j < p.rank ? v * scale : 0.0f);
             }
-            // (lane: row li, rank indices 8 (v / 4) + 4 g + v % 4)
-#pragma unroll
-            for (int n = 0; n < 4; ++n) *reinterpret_cast<f32x4*>(&part[wave][((2 * n + g) * 32 + li) * 4]) = f32x4{c[4 * n], c[4 * n + 1], c[4 * n + 2], c[4 * n + 3]};
-            __syncthreads();
-            // two values a thread: rows by lane, so that the sums are read without bank conflicts
-            const int row = (tid >> 1) & 31, q = tid >> 6, e0 = (tid & 1) * 2;
-            float s0 = 0.0f, s1 = 0.0f;
-#pragma unroll
-            for (int w8 = 0; w8 < 8; ++w8) {
-                const float* at = &part[w8][(q * 32 + row) * 4 + e0];
-                s0 += at[0];
-                s1 += at[1];
-            }
-            const int jj = j0 + 4 * q + e0;
-            if (((rows >> row) & 1) && row0 + row < p.rows && jj < r16) {
-                leave<T, true>(t, row0 + row, ld, jj, r16, jj < p.rank ? s0 * scale : 0.0f);
-                leave<T, true>(t, row0 + row, ld, jj + 1, r16, jj + 1 < p.rank ? s1 * scale : 0.0f);
-            }
-            __syncthreads();
         }
     }
 }
 
 // The projection of up to 16 RB rows: bound by reading the weight once.  A workgroup has 16 output columns, its eight waves share the
-// width, and every wave's weight loads (16 bytes a lane, 16 columns x 64 bytes an instruction) go straight to registers, several on their way.
+// width, and every wave's weight loads (16 bytes a lane, 16 columns x 64 bytes an instruction) go straight to registers, four or eight on
+// their way.
 // The waves' sums meet in LDS; a thread then has one column of a row, adds the row's adapter in fp32 and stores.
 template <typename T, int RB>
-__global__ __launch_bounds__(512) void skinny_kernel(const vpe_adapter_linear_args p, const float* __restrict__ t, int r16) {
+__global__ __launch_bounds__(512, 4) void skinny_kernel(const vpe_adapter_linear_args p, const float* __restrict__ t, int r16) {
     constexpr int STEP = sizeof(T) == 2 ? 32 : 16;            // width of an instruction group (four lanes of 16 bytes)
-    __shared__ __attribute__((aligned(16))) float part[8][RB * 256];
+    __shared__ __attribute__((aligned(16))) float part[WAVES][RB * 256];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col0 = blockIdx.x * 16, n = lane & 15, q = lane >> 4;
     const int col = col0 + n < p.out_features ? col0 + n : p.out_features - 1;
     const T* w = reinterpret_cast<const T*>(p.weight) + (int64_t)col * p.in_features + q * Elem<T>::CE;
@@ -138,19 +139,63 @@ __global__ __launch_bounds__(512) void skinny_kernel(const vpe_adapter_linear_ar
         x[b] = reinterpret_cast<const T*>(p.x) + (int64_t)r * p.x_row + q * Elem<T>::CE;
         acc[b] = f32x4{0, 0, 0, 0};
     }
-    // (in_features is a multiple of 64: whole steps; waves take them in turn)
-#pragma unroll 4
-    for (int k = wave * STEP; k < p.in_features; k += 8 * STEP) {
-        const u32x4 a = ld_global_16(w + k);
+    // (in_features is a multiple of 64: whole steps; waves take them in turn, AHEAD of them asked for before the first is used)
+    constexpr int AHEAD = RB == 1 ? 8 : 4;
+    u32x4 wv[AHEAD], xv[AHEAD][RB];
+    auto ask = [&](int k) {
 #pragma unroll
-        for (int b = 0; b < RB; ++b) {
-            const u32x4 c = ld_global_16(x[b] + k);
-            if constexpr (sizeof(T) == 2) {
-                acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, c), acc[b], 0, 0, 0);
-            } else {
-                const f32x4 fa = __builtin_bit_cast(f32x4, a), fc = __builtin_bit_cast(f32x4, c);
+        for (int u = 0; u < AHEAD; ++u) {
+            const int at = k + u * WAVES * STEP < p.in_features ? k + u * WAVES * STEP : k;
+            wv[u] = ld_global_16(w + at);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[e], fc[e], acc[b], 0, 0, 0);
+            for (int b = 0; b < RB; ++b) xv[u][b] = ld_global_16(x[b] + at);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const int k0 = wave * STEP;
+    if (k0 < p.in_features) ask(k0);
+    // the adapters' share of the values that this thread will store, bias included: its loads come behind the weight's first ones, not behind
+    // the product
+    constexpr int OUT = (RB * 256 + 64 * WAVES - 1) / (64 * WAVES);
+    float extra[OUT];
+#pragma unroll
+    for (int n = 0; n < OUT; ++n) {
+        const int o = tid + n * 64 * WAVES, row = o >> 4, c = col0 + (o & 15);
+        extra[n] = 0.0f;
+        if (o >= RB * 256 || row >= p.rows || c >= p.out_features) continue;
+        const int a = p.adapter ? p.adapter[row] : -1;
+        if (p.bias) extra[n] = p.bias[c];
+        if (a < 0 || a >= p.adapters) continue;
+        const T* up = reinterpret_cast<const T*>(p.b) + ((int64_t)a * p.out_features + c) * p.rank;
+        const float* low = t + (int64_t)row * r16;
+        float sum = 0.0f;
+#pragma unroll 2
+        for (int j = 0; j < p.rank; j += 8) {
+            float b[8];
+            unpack<T>(ld_global_16(up + j), b);
+            if (sizeof(T) == 4) unpack<T>(ld_global_16(up + j + 4), b + 4);
+            const f32x4 l0 = *reinterpret_cast<const f32x4*>(low + j), l1 = *reinterpret_cast<const f32x4*>(low + j + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = fmaf(l0[e], b[e], sum);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = fmaf(l1[e], b[4 + e], sum);
+        }
+        extra[n] += sum;
+    }
+    for (int k = k0; k < p.in_features; k += AHEAD * WAVES * STEP) {
+        if (k != k0) ask(k);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (k + u * WAVES * STEP >= p.in_features) break;
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                if constexpr (sizeof(T) == 2) {
+                    acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wv[u]), __builtin_bit_cast(bf16x8, xv[u][b]), acc[b], 0, 0, 0);
+                } else {
+                    const f32x4 fa = __builtin_bit_cast(f32x4, wv[u]), fc = __builtin_bit_cast(f32x4, xv[u][b]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[e], fc[e], acc[b], 0, 0, 0);
+                }
             }
         }
     }
@@ -158,28 +203,14 @@ __global__ __launch_bounds__(512) void skinny_kernel(const vpe_adapter_linear_ar
 #pragma unroll
     for (int b = 0; b < RB; ++b) *reinterpret_cast<f32x4*>(&part[wave][(b * 16 + n) * 16 + 4 * q]) = acc[b];
     __syncthreads();
-    for (int o = tid; o < RB * 256; o += 512) {
-        const int row = o >> 4, c = col0 + (o & 15);
-        if (row >= p.rows || c >= p.out_features) continue;
+#pragma unroll
+    for (int n2 = 0; n2 < OUT; ++n2) {
+        const int o = tid + n2 * 64 * WAVES, row = o >> 4, c = col0 + (o & 15);
+        if (o >= RB * 256 || row >= p.rows || c >= p.out_features) continue;
         float y = 0.0f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) y += part[k][o];
-        const int a = p.adapter ? p.adapter[row] : -1;
-        if (a >= 0 && a < p.adapters) {
-            const T* up = reinterpret_cast<const T*>(p.b) + ((int64_t)a * p.out_features + c) * p.rank;
-            const float* low = t + (int64_t)row * r16;
-            for (int j = 0; j < p.rank; j += 8) {
-                float b[8];
-                unpack<T>(ld_global_16(up + j), b);
-                if (sizeof(T) == 4) unpack<T>(ld_global_16(up + j + 4), b + 4);
-                const f32x4 l0 = *reinterpret_cast<const f32x4*>(low + j), l1 = *reinterpret_cast<const f32x4*>(low + j + 4);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y = fmaf(l0[e], b[e], y);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) y = fmaf(l1[e], b[4 + e], y);
-            }
-        }
-        if (p.bias) y += p.bias[c];
+        for (int k = 0; k < WAVES; ++k) y += part[k][o];
+        y += extra[n2];
         if (p.out_f32) reinterpret_cast<float*>(p.out)[row * p.out_row + c] = y;
         else reinterpret_cast<T*>(p.out)[row * p.out_row + c] = from_f32<T>(y);
     }
@@ -190,24 +221,20 @@ hipError_t launch(const vpe_adapter_linear_args& args, hipStream_t s) {
     vpe_adapter_linear_args a = args;
     if (a.adapters == 0 || !a.adapter) { a.adapters = 0; a.adapter = nullptr; }
     const int r16 = rank16(a);
-    const bool skinny = a.rows <= SKINNY_ROWS;
+    const bool skinny = a.rows <= skinny_rows<T>();
     if (a.adapter) {
-        const dim3 tasks((uint32_t)(((int64_t)a.rows * r16 + 3) / 4));
-        if (skinny) hipLaunchKernelGGL((adapter_rows_kernel<T, false>), tasks, dim3(256), 0, s, a, a.workspace, r16);
-        else if (a.rows <= 256) hipLaunchKernelGGL((adapter_rows_kernel<T, true>), tasks, dim3(256), 0, s, a, a.workspace, r16);
-        else hipLaunchKernelGGL(adapter_tiles_kernel<T>, dim3(cdiv(a.rows, 32)), dim3(512), 0, s, a, a.workspace, r16);
+        auto waves = [&](int rows, int indices) { return dim3((uint32_t)(((int64_t)cdiv(a.rows, rows) * (r16 / indices) + 3) / 4)); };
+        if (skinny) hipLaunchKernelGGL((adapter_down_kernel<T, false, 1, 1>), waves(1, 1), dim3(256), 0, s, a, a.workspace, r16);
+        else if (a.rows <= ONE_VALUE_ROWS) hipLaunchKernelGGL((adapter_down_kernel<T, true, 1, 1>), waves(1, 1), dim3(256), 0, s, a, a.workspace, r16);
+        else hipLaunchKernelGGL((adapter_down_kernel<T, true, 4, 8>), waves(4, 8), dim3(256), 0, s, a, a.workspace, r16);
         const hipError_t rc = hipGetLastError();
         if (rc != hipSuccess) return rc;
     }
     if (skinny) {
-        const dim3 grid(cdiv(a.out_features, 16)), block(512);
+        const dim3 grid(cdiv(a.out_features, 16)), block(64 * WAVES);
         const float* t = reinterpret_cast<const float*>(a.workspace);
-        switch (cdiv(a.rows, 16)) {
-            case 1: hipLaunchKernelGGL((skinny_kernel<T, 1>), grid, block, 0, s, a, t, r16); break;
-            case 2: hipLaunchKernelGGL((skinny_kernel<T, 2>), grid, block, 0, s, a, t, r16); break;
-            case 3: hipLaunchKernelGGL((skinny_kernel<T, 3>), grid, block, 0, s, a, t, r16); break;
-            default: hipLaunchKernelGGL((skinny_kernel<T, 4>), grid, block, 0, s, a, t, r16); break;
-        }
+        if (sizeof(T) == 2 || a.rows <= 16) hipLaunchKernelGGL((skinny_kernel<T, 1>), grid, block, 0, s, a, t, r16);
+        else hipLaunchKernelGGL((skinny_kernel<T, sizeof(T) == 2 ? 1 : 2>), grid, block, 0, s, a, t, r16);
         return hipGetLastError();
     }
     GemmArgs m{};

@@ -302,8 +302,10 @@ __device__ __forceinline__ void rowdot_epilogue_transposed(const GemmArgs& p, f3
 // infinities and NaN stay with its rows.  Operands come
 // straight from global memory: a lane has a row's, or a column's, eight elements of a 16-deep step.  (A tile of one adapter of rank 32 and
 // 256 x 256 takes 1.5 us for it, all latency: three dependent loads.)
-template <typename T, int MI, int NI>
-__device__ __forceinline__ void adapter_steps(const GemmArgs& p, f32x16 (&acc)[MI][NI], int row0, int col0, int lane) {
+// KG > 1: the groups of waves that hold a tile's partial sums take its adapters in turn (48 rows of 32 adapters, 4096 x 4096: 31 us with all
+// of them in group 0, XXX so).
+template <typename T, int MI, int NI, int KG>
+__device__ __forceinline__ void adapter_steps(const GemmArgs& p, f32x16 (&acc)[MI][NI], int row0, int col0, int lane, int kg) {
     const int g = lane >> 5, li = lane & 31, steps = (p.rank + 15) >> 4;
     struct Frag { f32x4 lo, hi; };                       // fp32: a step's eight elements; bf16 (lo alone): 16 bytes
     auto load = [&](const T* src) {
@@ -334,6 +336,7 @@ __device__ __forceinline__ void adapter_steps(const GemmArgs& p, f32x16 (&acc)[M
     };
     const Frag zero = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
     if (p.adapters == 0) return;
+    int turn = 0;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
         const int r = row0 + 32 * i + li < p.M ? row0 + 32 * i + li : p.M - 1;
@@ -345,6 +348,11 @@ __device__ __forceinline__ void adapter_steps(const GemmArgs& p, f32x16 (&acc)[M
             const bool mine = id == a;
             const uint64_t rows = __ballot(mine);
             todo &= ~rows;
+            if (KG > 1) {
+                const bool mine_now = turn == kg;
+                turn = turn + 1 == KG ? 0 : turn + 1;
+                if (!mine_now) continue;
+            }
             columns(a);
             // (a block's products in registers of their own: with the accumulators themselves carried through the step loop the compiler
             // keeps those of the large tiles in scratch)
@@ -745,8 +753,7 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, OCC * WGM * WGN * KG / 4) void
         }
     }
     constexpr int OUT = EPI == EPI_ADAPT ? EPI_STORE : EPI;
-    if constexpr (EPI == EPI_ADAPT)
-        if (kg == 0) adapter_steps<T, MI, NI>(p, acc, m0 + wm * WM, n0 + wn * WN, lane);
+    if constexpr (EPI == EPI_ADAPT) adapter_steps<T, MI, NI, KG>(p, acc, m0 + wm * WM, n0 + wn * WN, lane, kg);
     if constexpr (BLOCK) {                                    // (whole tile staged in LDS)
         block_epilogue<T, OUT, BM, BN, WGM, WGN, KG, AMODE == A_PLAIN && EPI != EPI_ADAPT>(p, acc, smem, lnrow, m0, n0);
     } else if constexpr (EPI == EPI_ROWDOT) {
