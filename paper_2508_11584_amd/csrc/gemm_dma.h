@@ -302,8 +302,8 @@ __device__ __forceinline__ void rowdot_epilogue_transposed(const GemmArgs& p, f3
 // infinities and NaN stay with its rows.  Operands come
 // straight from global memory: a lane has a row's, or a column's, eight elements of a 16-deep step.  (A tile of one adapter of rank 32 and
 // 256 x 256 takes 1.5 us for it, all latency: three dependent loads.)
-// KG > 1: the groups of waves that hold a tile's partial sums take its adapters in turn (48 rows of 32 adapters, 4096 x 4096: 31 us with all
-// of them in group 0, XXX so).
+// KG > 1: the groups of waves that hold a tile's partial sums take its adapters in turn (48 rows of 32 adapters, 4096 x 4096: a call is 35 us with
+// all of them in group 0, 24 so).
 template <typename T, int MI, int NI, int KG>
 __device__ __forceinline__ void adapter_steps(const GemmArgs& p, f32x16 (&acc)[MI][NI], int row0, int col0, int lane, int kg) {
     const int g = lane >> 5, li = lane & 31, steps = (p.rank + 15) >> 4;

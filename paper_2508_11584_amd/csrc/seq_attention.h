@@ -266,8 +266,8 @@ constexpr int seq_lds_bytes() {
 // of the rows and every KW-th tile; a row's KW results meet in LDS and are added in a fixed order.
 // A wave computes scores transposed, S^T = K Q^T: a lane holds half of one row's scores, reductions over the keys stay in the lane but for one
 // exchange, and the probabilities are the second product's operand, O^T = V^T P^T, as they lie.
-// An instantiation per kind of score (with all of them behind run-time branches a tile of slopes alone took 4300 clocks of a lone wave, now XXX; a
-// plain one takes 2100).
+// An instantiation per kind of score (with all of them behind run-time branches a tile of slopes alone took twice a plain one's time: ViT-B 518x518 32
+// us, so 25).
 template <typename T, int D, int KT, int QW, int KW, bool CAP, int DIST, int OCC>
 __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const vpe_attention_args p, const SeqAttnGrid grid) {
     using M = SeqMma<T, D>;
@@ -433,19 +433,23 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int v = 0; v < 16; ++v) sc[b][v] = 0.0f;
+        // Fragments are read two steps ahead of their products; left to itself the compiler reads each just before it is wanted, with a wait of
+        // 130 clocks
+        constexpr int SETS = sizeof(T) == 2 ? 3 : 1;
+        Frag k[SETS][NB];
+        auto read = [&](int ks) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
+            for (int b = 0; b < NB; ++b) k[ks % SETS][b] = M::k_frag(tile, 32 * b + li, ks, g);
+        };
+        if constexpr (SETS == 3) { read(0); read(1); }
 #pragma unroll
-            for (int b = 0; b < NB; ++b) sc[b] = M::mma(M::k_frag(tile, 32 * b + li, ks, g), q[ks], sc[b]);
-        if (sizeof(T) == 2) {                             // four fragments are read ahead of their products (7 % of a long causal call)
-            constexpr int AHEAD = 4;
-            __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+        for (int ks = 0; ks < KS; ++ks) {
+            if (SETS == 1) read(ks);
+            else if (ks + 2 < KS) read(ks + 2);
+            if (SETS == 3) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int n = 0; n < KS * NB - AHEAD; ++n) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+            for (int b = 0; b < NB; ++b) sc[b] = M::mma(k[ks % SETS][b], q[ks], sc[b]);
+            if (SETS == 3) __builtin_amdgcn_sched_barrier(0);
         }
     };
     // Is every score of the tile near zero, as caps go?
@@ -501,38 +505,60 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
     };
     // (plain scores stay raw: their factor and the reference are part of the exponentials' argument)
     auto exponent = [&](float s) { return PLAIN ? fmaf(s, scale2, -m) : s; };
-    auto finish = [&](f32x16 (&sc)[NB], const char* tile) {
+    // Takes the reference up by `by` (rows of which it is 0 stay).
+    auto rescale = [&](float by, float alpha) {
+        m += by;
+        l *= alpha;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) o[d][v] *= alpha;
+    };
+    // The largest probability that a lane has seen since the reference moved.  The reference is a row's maximum over its first tile; from then on
+    // nobody looks for a maximum before the exponentials, and when a probability has passed 2^30 it moves ahead of the next tile: up to there
+    // fp32 sums and bf16 probabilities are as precise as at 1, and a jump that overflows within one tile (2^97 times a row's largest so far)
+    // leaves sums that are not finite, which attention_row computes.  (Searching the maximum of every tile first took a lone wave 400 clocks of
+    // 2100 a tile, all latency: an exchange, a vote and a branch.)
+    constexpr float MOVE = 1073741824.0f;
+    float highest = 0.0f;
+    bool all_started = false;
+    auto begin_rows = [&](f32x16 (&sc)[NB]) {
         float rel = sc[0][0];
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int v = 0; v < 16; ++v) rel = fmaxf(rel, sc[b][v]);
         rel = exponent(halves_max(rel));
-        // the reference moves with a row's first key and when its maximum has grown by more than 8: until then probabilities stay below 2^8,
-        // and the wave skips the products with the accumulators
-        const bool grow = rel > 8.0f || (!started && rel > -INFINITY);
-        if (__any(grow)) {
-            const float by = grow ? rel : 0.0f, alpha = started ? __builtin_amdgcn_exp2f(-by) : 1.0f;
-            m += by;
-            l *= alpha;
+        const bool first = !started && rel > -INFINITY;
+        const float by = first ? rel : 0.0f;
+        m += by;                                          // (the row's sums are zero)
+        if constexpr (!PLAIN) {
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) o[d][v] *= alpha;
-            if constexpr (!PLAIN) {
-#pragma unroll
-                for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) sc[b][v] -= by;
-            }
+                for (int v = 0; v < 16; ++v) sc[b][v] -= by;
         }
-        started = started || rel > -INFINITY;
+        started = started | first;
+        all_started = __all(started | !real);
+    };
+    auto move_reference = [&] {
+        const float top = halves_max(highest);
+        const bool grow = top > MOVE;
+        const float by = grow ? __builtin_amdgcn_logf(top) : 0.0f;
+        rescale(by, grow ? __builtin_amdgcn_exp2f(-by) : 1.0f);
+        highest = 0.0f;
+    };
+    // Probabilities of the tile, their sums and the products with the values: STEPS steps of 16 keys a block.  The first block's fragments are read
+    // by the caller, ahead of the work on the scores, where there are registers for them (EARLY).
+    constexpr int BLOCKS = KT / 16 / M::STEPS;
+    constexpr bool EARLY = sizeof(T) == 2 && D == 64;
+    auto finish = [&](f32x16 (&sc)[NB], const typename M::Values& values, Frag (&f0)[M::STEPS][DB]) {
         __builtin_amdgcn_s_setprio(2);
-        const auto values = M::values(tile + TILE, lane);
-        auto block = [&](auto N) {                        // STEPS steps of 16 keys
+        auto block = [&](auto N) {
             constexpr int first = decltype(N)::value * M::STEPS;
-            Frag f[M::STEPS][DB];
-            M::template v_frags<first>(values, f);
+            Frag later[M::STEPS][DB];
+            constexpr bool here = decltype(N)::value > 0 || !EARLY;
+            if constexpr (here) M::template v_frags<first>(values, later);
 #pragma unroll
             for (int k = 0; k < M::STEPS; ++k) {
                 float e[8];
@@ -541,27 +567,38 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
                     e[n] = __builtin_amdgcn_exp2f(exponent(sc[(first + k) >> 1][8 * ((first + k) & 1) + n]));
                     l += e[n];
                 }
+#pragma unroll
+                for (int n = 0; n < 8; n += 2) highest = fmaxf(fmaxf(highest, e[n]), e[n + 1]);
                 const Frag b = M::probs(e);
 #pragma unroll
-                for (int d = 0; d < DB; ++d) o[d] = M::mma(f[k][d], b, o[d]);
+                for (int d = 0; d < DB; ++d) {
+                    if constexpr (here) o[d] = M::mma(later[k][d], b, o[d]);
+                    else o[d] = M::mma(f0[k][d], b, o[d]);
+                }
             }
         };
-        constexpr int BLOCKS = KT / 16 / M::STEPS;
         block(std::integral_constant<int, 0>{});
         if constexpr (BLOCKS > 1) block(std::integral_constant<int, 1>{});
         if constexpr (BLOCKS > 2) block(std::integral_constant<int, 2>{});
         if constexpr (BLOCKS > 3) block(std::integral_constant<int, 3>{});
         __builtin_amdgcn_s_setprio(0);
     };
-    auto compute = [&](const char* stage, int t) {
+    // Tile t, with `loads` (the next tile's) issued while the first products run: the CU's one address unit takes 16 clocks for each of them, and a
+    // wave that waits for it issues nothing else.
+    auto compute = [&](const char* stage, int t, auto&& loads) {
         const char* tile = stage + kw * OWN;
         const int j0 = j_begin + t * KT;
-        if (j0 >= lim_max) return;                        // (the wave's rows see nothing of it)
+        if (j0 >= lim_max) { loads(); return; }           // (the wave's rows see nothing of it)
         const bool masked = j0 + KT > lim_min || j0 + KT > j_end;
         f32x16 sc[NB];
         __builtin_amdgcn_s_setprio(1);                    // (of a SIMD's waves the one with products to issue goes first)
         tile_scores(sc, tile);
+        loads();
         __builtin_amdgcn_s_setprio(0);
+        const auto values = M::values(tile + TILE, lane);
+        Frag f0[M::STEPS][DB];
+        if constexpr (EARLY) M::template v_frags<0>(values, f0);
+        if (__any(highest > MOVE)) move_reference();
         if constexpr (!PLAIN) shape(sc, tile, j0);
         if (masked) {
             const int left = (limit < j_end ? limit : j_end) - j0 - 4 * g;
@@ -571,7 +608,8 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
                 for (int v = 0; v < 16; ++v)
                     if (32 * b + 8 * (v >> 2) + (v & 3) >= left) sc[b][v] = -INFINITY;
         }
-        finish(sc, tile);
+        if (!all_started) begin_rows(sc);
+        finish(sc, values, f0);
     };
 
     if constexpr (QW > 1) {
@@ -581,8 +619,9 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
         __builtin_amdgcn_s_waitcnt(0x0F70);               // vmcnt(0): the loads into LDS have landed
         __syncthreads();
         for (int it = 0; it < turns; ++it) {
-            if (it + 1 < turns) dma(smem + ((it + 1) & 1) * STAGE, it + 1);
-            if (KW == 1 || it * KW + kw < tiles) compute(smem + (it & 1) * STAGE, it * KW + kw);
+            auto loads = [&] { if (it + 1 < turns) dma(smem + ((it + 1) & 1) * STAGE, it + 1); };
+            if (KW == 1 || it * KW + kw < tiles) compute(smem + (it & 1) * STAGE, it * KW + kw, loads);
+            else loads();
             __builtin_amdgcn_s_waitcnt(0x0F70);
             __syncthreads();
         }
@@ -599,7 +638,7 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
                 __builtin_amdgcn_s_waitcnt(0x0F70);
             }
             asm volatile("" ::: "memory");
-            compute(smem + buf * STAGE, t);
+            compute(smem + buf * STAGE, t, [] {});
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_waitcnt(vmcnt_imm(63) & ~0x0F00);      // (its reads are done: the next loads may land there)
         }
