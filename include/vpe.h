@@ -52,7 +52,7 @@ typedef enum { VPE_OK = 0, VPE_SKIPPED = 1, VPE_BUSY = 2, VPE_EINVAL = -1, VPE_E
                VPE_EHIP = -4 } vpe_status;
 typedef enum { VPE_F32 = 0, VPE_BF16 = 1 } vpe_dtype;
 typedef enum { VPE_MLP_GELU = 0, VPE_MLP_SWIGLU = 1 } vpe_mlp;
-typedef enum { VPE_HEAD_SEG = 0, VPE_HEAD_DEPTH = 1, VPE_HEAD_DET = 2, VPE_HEAD_DPT = 3 } vpe_head_kind;
+typedef enum { VPE_HEAD_SEG = 0, VPE_HEAD_DEPTH = 1, VPE_HEAD_DET = 2, VPE_HEAD_DPT = 3, VPE_HEAD_QUERY = 4 } vpe_head_kind;
 
 enum {
     VPE_FLAG_GRAPHS = 1,     /* replay the encoder and the heads as captured HIP graphs */
@@ -143,12 +143,20 @@ typedef struct {
  *                  c2_b,) unit b: c1_w, c1_b, c2_w, c2_b, out_w [F][F], out_b; head1_w [F/2][F][3][3], head1_b;
  *                  head2_w [32][F/2][3][3], head2_b; head3_w [1][32], head3_b [1].
  *                  outputs: 0 = depth fp32 [B][img_h][img_w].
+ *   VPE_HEAD_QUERY learned queries that read the final map (all its rows: CLS, registers, patches), per image and query a row
+ *                  of class logits, by the operators for packed requests below.  t = query, q = t q_w^T + q_b;
+ *                  k, v = the two halves of the map's rows times kv_w^T + kv_b (plus the image's adapter, vpe_set_head_adapters);
+ *                  o = attention of q over the image's k and v, dim / 64 heads of 64, scores times 1/8;
+ *                  x = t + ls1 (o out_w^T + out_b); logits = LayerNorm(x) cls_w^T + cls_b.
+ *                  weights: query [channels][dim], q_w [dim][dim], q_b [dim], kv_w [2 dim][dim], kv_b, out_w [dim][dim], out_b,
+ *                  ls1 [dim], norm_g, norm_b, cls_w [classes][dim], cls_b.
+ *                  outputs: 0 = logits fp32 [B][channels][classes].
  *   every_n >= 1: the head runs on frame f iff f % every_n == 0 (paper, Sec. "Dynamic Frequency Control").
  */
 typedef struct {
     int32_t kind;         /* vpe_head_kind */
-    int32_t classes;      /* seg: C; det: number of object classes; depth, dpt: ignored */
-    int32_t channels;     /* det / depth / dpt hidden width (multiple of 64; dpt: at most 256); seg: ignored */
+    int32_t classes;      /* seg, query: C; det: number of object classes; depth, dpt: ignored */
+    int32_t channels;     /* det / depth / dpt hidden width (multiple of 64; dpt: at most 256); query: queries an image, 1..256; seg: ignored */
     int32_t every_n;
     const void* weights;  /* host, fp32 */
     uint64_t weights_bytes;
@@ -319,7 +327,8 @@ int vpe_run_head(vpe_engine* e, int head, vpe_feat fh, void* stream);
  *     process ends) instead of from the engine's workspace;
  *   - the head's kernels are always launched one by one (never as a graph replay, even with VPE_FLAG_GRAPHS), and
  *     the call performs no hipMalloc / hipFree / graph instantiation.
- * Supported heads: VPE_HEAD_SEG (needs none), VPE_HEAD_DET (batch * patches * 2 channels elements), VPE_HEAD_DEPTH
+ * Supported heads: VPE_HEAD_SEG (needs none), VPE_HEAD_DET (batch * patches * 2 channels elements), VPE_HEAD_QUERY
+ * (about batch * tokens * (2 dim elements + 512 bytes)), VPE_HEAD_DEPTH
  * (about 129 * batch * patches * channels elements); a head whose buffers exceed 8 MiB and VPE_HEAD_DPT are
  * refused with VPE_EINVAL and a message that states both sizes.  Nothing in the array needs clearing (a run writes
  * every element before it reads it), and it keeps the last run's contents.  All calls on one GPU share the array:
@@ -422,6 +431,13 @@ int vpe_stage_times(vpe_engine* e, float* encode_ms, float* head_ms, int n);
  * (no activation; mlp_hidden columns): 9 + 8 against 6 is what the fusion saves.
  * Also reports the algorithmic flops and bytes of one launch. */
 int vpe_time_kernel(vpe_engine* e, int which, int reps, float* ms_per_launch, double* flops, double* bytes);
+
+/* Low-rank adapters of a VPE_HEAD_QUERY head's kv projection: image i of a batch has adapter adapter_of_image[i] (HOST array
+ * [batch]; outside 0 .. adapters - 1: none).  a [adapters][rank][dim], b [adapters][2 dim][rank] in the engine's dtype and scale
+ * [adapters] in fp32 (null: 1) are DEVICE memory as vpe_adapter_linear takes it, read by every later run and to be kept until the
+ * next call or vpe_destroy; adapters 0 takes them away.  Blocks until the head's last run has finished; a set-up call. */
+int vpe_set_head_adapters(vpe_engine* e, int head, int adapters, int rank, const void* a, const void* b, const float* scale,
+                          const int32_t* adapter_of_image);
 
 /* Message of the most recent failure of a call on this engine (engine may be NULL: the last failure of a call
  * that had no engine, on this thread).  Borrowed; valid until the next failing call. */

@@ -16,7 +16,7 @@ import numpy as np
 VPE_OK, VPE_SKIPPED, VPE_BUSY, VPE_EINVAL, VPE_ENOMEM, VPE_ESTALE, VPE_EHIP = 0, 1, 2, -1, -2, -3, -4
 VPE_F32, VPE_BF16 = 0, 1
 VPE_MLP_GELU, VPE_MLP_SWIGLU = 0, 1
-VPE_HEAD_SEG, VPE_HEAD_DEPTH, VPE_HEAD_DET, VPE_HEAD_DPT = 0, 1, 2, 3
+VPE_HEAD_SEG, VPE_HEAD_DEPTH, VPE_HEAD_DET, VPE_HEAD_DPT, VPE_HEAD_QUERY = 0, 1, 2, 3, 4
 VPE_NORM_NONE, VPE_NORM_LAYER, VPE_NORM_RMS = 0, 1, 2
 VPE_FLAG_GRAPHS, VPE_FLAG_HOST_ONLY, VPE_FLAG_WALL_CLOCK, VPE_FLAG_TIMING = 1, 2, 4, 8
 
@@ -94,6 +94,7 @@ def load_library(path: Optional[str] = None):
     L.vpe_encode_at.argtypes = [vp, vp, vp, C.c_double, C.POINTER(vpe_feat)]
     L.vpe_set_head_rate_hz.argtypes = [vp, i32, C.c_double]
     L.vpe_feat_view.argtypes = [vp, vpe_feat, i32, C.POINTER(vp), i64p]
+    L.vpe_set_head_adapters.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp]
     L.vpe_head_output.argtypes = [vp, i32, i32, C.POINTER(vp), i64p]
     L.vpe_sync.argtypes = [vp]
     L.vpe_head_done.argtypes = [vp, i32]
@@ -110,7 +111,7 @@ def load_library(path: Optional[str] = None):
     L.vpe_last_error.restype = C.c_char_p
     L.vpe_destroy.argtypes = [vp]
     L.vpe_destroy.restype = None
-    for n in ("vpe_workspace_bytes", "vpe_create", "vpe_encode", "vpe_encode_at", "vpe_run_head", "vpe_set_head_rate",
+    for n in ("vpe_workspace_bytes", "vpe_create", "vpe_encode", "vpe_encode_at", "vpe_run_head", "vpe_set_head_rate", "vpe_set_head_adapters",
               "vpe_set_head_rate_hz", "vpe_preprocess_u8", "vpe_attention_workspace_bytes", "vpe_attention", "vpe_block_norm",
               "vpe_adapter_linear_workspace_bytes", "vpe_adapter_linear", "vpe_next_encode_stream", "vpe_feat_view",
               "vpe_head_output", "vpe_sync", "vpe_run_head_static", "vpe_head_done", "vpe_wait_head", "vpe_stage_times", "vpe_stats", "vpe_time_kernel", "vpe_run_head_latest", "vpe_head_counters", "vpe_frame_ready"):
@@ -455,6 +456,13 @@ def vpe_set_head_rate_hz(engine, head: int, max_hz: float) -> None:
         raise VpeError(rc, vpe_last_error(engine))
 
 
+def vpe_set_head_adapters(engine, head: int, adapters: int, rank: int, a_ptr, b_ptr, scale_ptr, adapter_of_image: Sequence[int]) -> None:
+    rc = lib().vpe_set_head_adapters(engine, head, adapters, rank, a_ptr, b_ptr, scale_ptr,
+                                     (C.c_int32 * len(adapter_of_image))(*adapter_of_image) if adapters else None)
+    if rc:
+        raise VpeError(rc, vpe_last_error(engine))
+
+
 def vpe_feat_view(engine, fh: vpe_feat, tap: int):
     ptr = C.c_void_p()
     shape = (C.c_int64 * 3)()
@@ -560,6 +568,7 @@ class Engine:
             harr[i].weights_bytes = blob.nbytes
         self.cfg, self.head_arr = cfg, harr
         self.host_only = bool(flags & VPE_FLAG_HOST_ONLY)
+        self._adapters = {}                       # head -> the tensors that its runs read
         self.dtype = dtype
         self.workspace_bytes = vpe_workspace_bytes(cfg, harr, self.n_heads)
         self._ws = None
@@ -607,6 +616,21 @@ class Engine:
     def set_head_rate_hz(self, head: int, max_hz: float) -> None:
         vpe_set_head_rate_hz(self.handle, head, max_hz)
 
+    def set_head_adapters(self, head: int, a=None, b=None, adapter_of_image: Sequence[int] = (), scale=None) -> None:
+        """Adapters of a query head's kv projection: a [adapters, rank, dim], b [adapters, 2 dim, rank] in the engine's dtype, scale float32
+        [adapters]; adapter_of_image [batch], -1 for none.  Kept by the engine until the next call; without arguments they are taken away."""
+        if a is None:
+            vpe_set_head_adapters(self.handle, head, 0, 0, None, None, None, ())
+        else:
+            _types()
+            dtype, dim = _bf16 if self.dtype == VPE_BF16 else _f32, self.cfg.dim
+            if a.dim() != 3 or len(adapter_of_image) != self.cfg.batch:
+                _refuse("a must be [adapters, rank, dim], adapter_of_image one index an image")
+            n, rank, device = a.shape[0], a.shape[1], self._ws.get_device() if self._ws is not None else a.get_device()
+            ptrs = (_ptr("a", a, device, dtype, (n, rank, dim)), _ptr("b", b, device, dtype, (n, 2 * dim, rank)), _ptr("scale", scale, device, _f32, (n,)))
+            vpe_set_head_adapters(self.handle, head, n, rank, *ptrs, adapter_of_image)
+        self._adapters[head] = (a, b, scale)
+
     def sync(self) -> None:
         vpe_sync(self.handle)
 
@@ -647,7 +671,7 @@ class Engine:
         kind = self.head_arr[head].kind
         is_map = which == 1 and kind in (VPE_HEAD_SEG, VPE_HEAD_DET)
         shape = [s for s in shape]
-        while len(shape) > 1 and shape[-1] == 1 and len(shape) > (3 if (is_map or kind in (VPE_HEAD_DEPTH, VPE_HEAD_DPT)) else 4):
+        while len(shape) > 1 and shape[-1] == 1 and len(shape) > (3 if (is_map or kind in (VPE_HEAD_DEPTH, VPE_HEAD_DPT, VPE_HEAD_QUERY)) else 4):
             shape.pop()
         return self._as_tensor(ptr, shape, torch.uint8 if is_map else torch.float32)
 

@@ -14,7 +14,9 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <memory>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -109,6 +111,19 @@ struct Dpt {
     int rh[5] = {}, rw[5] = {};    // their output sizes
 };
 
+// Constants and adapters of a head of learned queries.
+struct Query {
+    float* t = nullptr;            // [B Q][D] the queries as the residual stream takes them
+    void* q = nullptr;             // [B Q][D] projected
+    void *kv_w = nullptr, *out_w = nullptr, *cls_w = nullptr;
+    float *kv_b = nullptr, *out_b = nullptr, *cls_b = nullptr, *ls = nullptr, *norm_g = nullptr, *norm_b = nullptr;
+    int32_t *q_off = nullptr, *k_off = nullptr;   // [B + 1] first rows of the images
+    int32_t* adapter = nullptr;    // [B N] of the map's rows
+    int adapters = 0, rank = 0;
+    const void *a = nullptr, *b = nullptr;        // the caller's
+    const float* scale = nullptr;
+};
+
 // Intermediate buffers of a seg / det / DPT-lite head run (neither its input, the feature slot, nor its outputs):
 // normally part of the engine's workspace, or carved out of the library's static device array for
 // vpe_run_head_static.  Every element a run reads is written earlier in the same run; nothing relies on old contents.
@@ -117,11 +132,16 @@ struct HeadScratch {
     void* p[4] = {};               // depth: tap projections [B P][ch]
     void *z = nullptr, *r = nullptr;   // depth: stage input / convolution output [B 64 P][ch], reused across stages
     float* d8 = nullptr;           // depth: [pixel][ch / 64] partial 1-channel projections on the 8x grid
+    void *kv = nullptr, *att = nullptr, *o = nullptr, *n = nullptr;   // query: keys and values [B N][2 D], then [B Q][D]: attended, projected, normed
+    float* x = nullptr;            // query: [B Q][D]
+    void* work = nullptr;          // query: workspace of its operators, which run one after the other
+    uint64_t work_bytes = 0;
 };
 
 struct Head {
     int kind = 0, classes = 0, ch = 0, every_n = 1;
     Dpt dpt;
+    Query query;
     HeadScratch sc;
     // weights
     void* w0 = nullptr;            // seg: [C][D]; det: towers [2ch][9D]; depth: unused
@@ -135,7 +155,7 @@ struct Head {
     float* out_w = nullptr;
     float out_b = 0.0f;
     // activations / outputs
-    float* logits = nullptr;       // seg [B P][C]; det [B P][classes + 4]
+    float* logits = nullptr;       // seg [B P][C]; det [B P][classes + 4]; query [B Q][C]
     uint8_t* classmap = nullptr;
     float* depth = nullptr;
     // scheduling
@@ -248,6 +268,7 @@ int64_t head_floats(const vpe_backbone_cfg& c, const vpe_head_cfg& h) {
             n += 14 * (F * F * 9 + F) + 4 * (F * F + F);                                    // 7 residual units, 4 output 1x1
             return n + (F / 2) * F * 9 + F / 2 + 32 * (F / 2) * 9 + 32 + 32 + 1;
         }
+        case VPE_HEAD_QUERY: return ch * D + 4 * (D * D + D) + 3 * D + (int64_t)h.classes * D + h.classes;
     }
     return -1;
 }
@@ -283,12 +304,13 @@ std::string validate(const vpe_backbone_cfg* c, const vpe_head_cfg* heads, int n
     }
     for (int i = 0; i < n_heads; ++i) {
         const vpe_head_cfg& h = heads[i];
-        if (h.kind != VPE_HEAD_SEG && h.kind != VPE_HEAD_DEPTH && h.kind != VPE_HEAD_DET && h.kind != VPE_HEAD_DPT)
+        if (h.kind != VPE_HEAD_SEG && h.kind != VPE_HEAD_DEPTH && h.kind != VPE_HEAD_DET && h.kind != VPE_HEAD_DPT && h.kind != VPE_HEAD_QUERY)
             return "unknown head kind";
         if (h.kind == VPE_HEAD_DPT && h.channels > 256) return "a DPT head takes channels in 64..256";
         if (h.every_n < 1) return "every_n must be >= 1";
-        if ((h.kind == VPE_HEAD_SEG || h.kind == VPE_HEAD_DET) && (h.classes < 1 || h.classes > 256)) return "classes must be in 1..256";
-        if (h.kind != VPE_HEAD_SEG && (h.channels < 64 || h.channels % 64 || h.channels > 1024))
+        if (h.kind == VPE_HEAD_QUERY && (h.channels < 1 || h.channels > 256)) return "a query head takes 1..256 queries in channels";
+        if ((h.kind == VPE_HEAD_SEG || h.kind == VPE_HEAD_DET || h.kind == VPE_HEAD_QUERY) && (h.classes < 1 || h.classes > 256)) return "classes must be in 1..256";
+        if (h.kind != VPE_HEAD_SEG && h.kind != VPE_HEAD_QUERY && (h.channels < 64 || h.channels % 64 || h.channels > 1024))
             return "channels must be a multiple of 64 in 64..1024";
         if (!h.weights) return "head weights pointer is null";
         if ((int64_t)h.weights_bytes != 4 * head_floats(*c, h)) {
@@ -352,6 +374,10 @@ double head_flops(const vpe_engine& e, const Head& h) {
             // residual units on the 1/4, 1, 4, 16 grids, the output convolutions on the 64x and 196x grids
             return P * (7.5 * e.D * F + 9.0 * F * F * (2 * 0.25 + 4 * 1 + 4 * 4 + 4 * 16) + 9.0 * F * F / 2 * 64 + 9.0 * 64 * 64 * 196);
         }
+        case VPE_HEAD_QUERY: {
+            const double D = e.D, BQ = (double)e.B * h.ch;
+            return 2.0 * e.T * D * D + BQ * (2.0 * e.N * D + D * D + D * h.classes);
+        }
         default: return P * (4.0 * e.D * h.ch + 85.0 * 9 * h.ch * h.ch);   // four 3x3 stages on 1 + 4 + 16 + 64 grids
     }
 }
@@ -359,11 +385,35 @@ double head_flops(const vpe_engine& e, const Head& h) {
 // About what a head's run takes by itself, in us: its launches (about 5 us each when they are small) and its operations at 600
 // TFLOP/s (fp32: a tenth); head_flops counts multiply-adds.
 double head_us(const vpe_engine& e, const Head& h) {
-    const int launches = h.kind == VPE_HEAD_SEG ? 2 : h.kind == VPE_HEAD_DET ? 3 : h.kind == VPE_HEAD_DPT ? 35 : 10;
+    const int launches = h.kind == VPE_HEAD_SEG ? 2 : h.kind == VPE_HEAD_DET ? 3 : h.kind == VPE_HEAD_DPT ? 35 : h.kind == VPE_HEAD_QUERY ? 6 : 10;
     return 5.0 * launches + 2.0 * head_flops(e, h) / (e.bf ? 600e6 : 60e6);
 }
 
-// Hands out the intermediate buffers of a seg / det / DPT-lite head (see HeadScratch) from `b`.
+// The calls of a query head's run, without what changes from run to run.
+vpe_adapter_linear_args query_projection(const vpe_engine& e, const void* x, const void* w, const float* bias, int rows, int n, void* out, bool out_f32 = false) {
+    vpe_adapter_linear_args a{};
+    a.dtype = e.cfg.dtype; a.out_f32 = out_f32;
+    a.rows = rows; a.in_features = e.D; a.out_features = n;
+    a.x = x; a.weight = w; a.bias = bias; a.out = out;
+    a.x_row = e.D; a.out_row = n;
+    return a;
+}
+
+vpe_attention_args query_attention(const vpe_engine& e, const Head& h) {
+    vpe_attention_args a{};
+    a.dtype = e.cfg.dtype; a.head_dim = 64; a.heads = a.kv_heads = e.nh;
+    a.sequences = e.B; a.max_q = h.ch; a.max_k = e.N;
+    a.q_rows = e.B * h.ch; a.k_rows = e.T;
+    a.scale = 0.125f;
+    a.q_row = a.out_row = e.D; a.k_row = a.v_row = 2 * e.D;
+    a.q_head = a.k_head = a.v_head = a.out_head = 64;
+    a.q = h.query.q; a.q_offsets = h.query.q_off; a.k_offsets = h.query.k_off;
+    return a;
+}
+
+constexpr int QUERY_RANK = 128;    // the largest rank of an adapter: workspace is there for it from the start
+
+// Hands out the intermediate buffers of a seg / det / DPT-lite / query head (see HeadScratch) from `b`.
 void place_head_scratch(const vpe_engine& e, const Head& h, Bump& b, HeadScratch& sc) {
     const uint64_t esz = e.esz, ch = h.ch, BP = (uint64_t)e.B * e.P;
     if (h.kind == VPE_HEAD_DET) {
@@ -373,6 +423,17 @@ void place_head_scratch(const vpe_engine& e, const Head& h, Bump& b, HeadScratch
         sc.z = b.take(BP * 64 * ch * esz);
         sc.r = b.take(BP * 64 * ch * esz);
         sc.d8 = (float*)b.take(4 * (ch / 64) * BP * 64);
+    } else if (h.kind == VPE_HEAD_QUERY) {
+        const uint64_t T = e.T, D = e.D, BQ = e.B * ch;
+        sc.kv = b.take(T * 2 * D * esz);
+        sc.att = b.take(BQ * D * esz);
+        sc.o = b.take(BQ * D * esz);
+        sc.n = b.take(BQ * D * esz);
+        sc.x = (float*)b.take(4 * BQ * D);
+        vpe_adapter_linear_args kv = query_projection(e, nullptr, nullptr, nullptr, e.T, 2 * e.D, nullptr);
+        kv.adapters = 1; kv.rank = QUERY_RANK;
+        sc.work_bytes = std::max(adapter_linear_workspace(kv), plan_seq_attention(query_attention(e, h)).workspace);
+        sc.work = b.take(sc.work_bytes);
     }
 }
 
@@ -426,6 +487,18 @@ void layout(vpe_engine& e, Bump& b) {
             place_head_scratch(e, h, b, h.sc);
             h.logits = f32(BP * (h.classes + 4));
             h.classmap = (uint8_t*)b.take(BP);
+        } else if (h.kind == VPE_HEAD_QUERY) {
+            Query& y = h.query;
+            const uint64_t BQ = B * ch, C = h.classes;
+            y.t = f32(BQ * D); y.q = b.take(BQ * D * esz);
+            y.kv_w = b.take(2 * D * D * esz); y.kv_b = f32(2 * D);
+            y.out_w = b.take(D * D * esz); y.out_b = f32(D);
+            y.ls = f32(D); y.norm_g = f32(D); y.norm_b = f32(D);
+            y.cls_w = b.take(C * D * esz); y.cls_b = f32(C);
+            y.q_off = (int32_t*)b.take(4 * (B + 1)); y.k_off = (int32_t*)b.take(4 * (B + 1));
+            y.adapter = (int32_t*)b.take(4 * T);
+            place_head_scratch(e, h, b, h.sc);
+            h.logits = f32(BQ * C);
         } else if (h.kind == VPE_HEAD_DPT) {
             Dpt& d = h.dpt;
             const uint64_t F = d.F;
@@ -594,6 +667,31 @@ int upload_head(vpe_engine& e, Head& h, const float* blob, int64_t n, float* sta
         TRY(up.f32(h.b1, h.classes));
         TRY(up.relayout((int64_t)4 * ch, h.w1, 4, ch, ch, 1, 0, 0, 0, 2 * ch, h.classes, ch));
         TRY(up.f32(h.b1 + h.classes, 4));
+    } else if (h.kind == VPE_HEAD_QUERY) {
+        Query& y = h.query;
+        const int B = e.B;
+        const float* t = up.take((int64_t)ch * D);
+        const float* qw = up.take((int64_t)D * D);
+        const float* qb = up.take(D);
+        std::vector<float> q((size_t)ch * D);
+        for (int i = 0; i < ch; ++i)
+            for (int n = 0; n < D; ++n) {
+                double acc = qb[n];
+                for (int k = 0; k < D; ++k) acc += (double)t[(int64_t)i * D + k] * qw[(int64_t)n * D + k];
+                q[(size_t)i * D + n] = (float)acc;
+            }
+        for (int b = 0; b < B; ++b) {
+            HIPCHK(&e, hipMemcpy(y.t + (int64_t)b * ch * D, t, 4 * q.size(), hipMemcpyHostToDevice));
+            TRY(up.relayout_host(q.data(), (int64_t)ch * D, (char*)y.q + (int64_t)b * ch * D * e.esz, ch, D, D, 1, 0, 0, 0, D, 0, 0));
+        }
+        TRY(up.relayout(2 * (int64_t)D * D, y.kv_w, 2 * D, D, D, 1, 0, 0, 0, D, 0, 0)); TRY(up.f32(y.kv_b, 2 * D));
+        TRY(up.relayout((int64_t)D * D, y.out_w, D, D, D, 1, 0, 0, 0, D, 0, 0)); TRY(up.f32(y.out_b, D));
+        TRY(up.f32(y.ls, D)); TRY(up.f32(y.norm_g, D)); TRY(up.f32(y.norm_b, D));
+        TRY(up.relayout((int64_t)h.classes * D, y.cls_w, h.classes, D, D, 1, 0, 0, 0, D, 0, 0)); TRY(up.f32(y.cls_b, h.classes));
+        std::vector<int32_t> off[2];
+        for (int b = 0; b <= B; ++b) { off[0].push_back(b * ch); off[1].push_back(b * e.N); }
+        HIPCHK(&e, hipMemcpy(y.q_off, off[0].data(), 4 * off[0].size(), hipMemcpyHostToDevice));
+        HIPCHK(&e, hipMemcpy(y.k_off, off[1].data(), 4 * off[1].size(), hipMemcpyHostToDevice));
     } else if (h.kind == VPE_HEAD_DPT) {
         Dpt& d = h.dpt;
         const int F = d.F;
@@ -900,10 +998,37 @@ int enqueue_dpt(vpe_engine& e, Head& h, int slot, hipStream_t s) {
     return 0;
 }
 
+int enqueue_query(vpe_engine& e, Head& h, const HeadScratch& sc, const void* map, hipStream_t s) {
+    const Query& y = h.query;
+    const int D = e.D, BQ = e.B * h.ch;
+    vpe_adapter_linear_args kv = query_projection(e, map, y.kv_w, y.kv_b, e.T, 2 * D, sc.kv);
+    if (y.adapters) {
+        kv.adapters = y.adapters; kv.rank = y.rank;
+        kv.a = y.a; kv.b = y.b; kv.adapter = y.adapter; kv.scale = y.scale;
+        kv.workspace = sc.work; kv.workspace_bytes = sc.work_bytes;
+    }
+    HIPCHK(&e, launch_adapter_linear(kv, s));
+    vpe_attention_args att = query_attention(e, h);
+    att.k = sc.kv; att.v = (const char*)sc.kv + (int64_t)D * e.esz; att.out = sc.att;
+    att.workspace = sc.work; att.workspace_bytes = sc.work_bytes;
+    HIPCHK(&e, launch_seq_attention(att, plan_seq_attention(att), s));
+    HIPCHK(&e, launch_adapter_linear(query_projection(e, sc.att, y.out_w, y.out_b, BQ, D, sc.o), s));
+    vpe_block_norm_args norm{};
+    norm.dtype = e.cfg.dtype; norm.rows = BQ; norm.dim = D; norm.requests = 1;
+    norm.post = VPE_NORM_NONE; norm.pre = VPE_NORM_LAYER; norm.residual_scale = 1.0f; norm.eps = e.cfg.ln_eps;
+    norm.x = y.t; norm.branch = sc.o; norm.out = sc.x; norm.normed = sc.n;
+    norm.x_row = norm.branch_row = norm.out_row = norm.normed_row = D;
+    norm.layer_scale = y.ls; norm.pre_gain = y.norm_g; norm.pre_bias = y.norm_b;
+    HIPCHK(&e, launch_block_norm(norm, s));
+    HIPCHK(&e, launch_adapter_linear(query_projection(e, sc.n, y.cls_w, y.cls_b, BQ, h.classes, h.logits, true), s));
+    return 0;
+}
+
 int enqueue_head_body(vpe_engine& e, Head& h, const HeadScratch& sc, int slot, hipStream_t s) {
     const int dt = e.bf, BP = e.B * e.P;
     void* const* f = &e.feat[slot * 4];
     if (h.kind == VPE_HEAD_DPT) return enqueue_dpt(e, h, slot, s);
+    if (h.kind == VPE_HEAD_QUERY) return enqueue_query(e, h, sc, f[3], s);
     if (h.kind == VPE_HEAD_SEG) {
         GemmArgs a = tokens_gemm(e, f[3], h.w0, h.b0, h.classes);
         a.out = h.logits; a.ldo = h.classes; a.out_f32 = 1;
@@ -1418,8 +1543,40 @@ int vpe_head_output(vpe_engine* e, int head, int which, const void** dev_ptr, in
     else if (h.kind == VPE_HEAD_SEG && which == 1) { *dev_ptr = h.classmap; shape[1] = e->H; shape[2] = e->W; }
     else if (h.kind == VPE_HEAD_DET && which == 0) { *dev_ptr = h.logits; shape[1] = e->gh; shape[2] = e->gw; shape[3] = h.classes + 4; }
     else if (h.kind == VPE_HEAD_DET && which == 1) { *dev_ptr = h.classmap; shape[1] = e->gh; shape[2] = e->gw; }
+    else if (h.kind == VPE_HEAD_QUERY && which == 0) { *dev_ptr = h.logits; shape[1] = h.ch; shape[2] = h.classes; }
     else if ((h.kind == VPE_HEAD_DEPTH || h.kind == VPE_HEAD_DPT) && which == 0) { *dev_ptr = h.depth; shape[1] = e->H; shape[2] = e->W; }
     else return e->fail(VPE_EINVAL, "this head has no such output");
+    return VPE_OK;
+}
+
+int vpe_set_head_adapters(vpe_engine* e, int head, int adapters, int rank, const void* a, const void* b, const float* scale,
+                          const int32_t* adapter_of_image) {
+    if (!e) return VPE_EINVAL;
+    if (head < 0 || head >= (int)e->heads.size()) return e->fail(VPE_EINVAL, "unknown head");
+    Head& h = e->heads[head];
+    if (h.kind != VPE_HEAD_QUERY) return e->fail(VPE_EINVAL, "this head takes no adapters");
+    if (adapters < 0) return e->fail(VPE_EINVAL, "adapters must not be negative");
+    if (adapters > 0) {
+        if (rank < 8 || rank % 8 || rank > QUERY_RANK) return e->fail(VPE_EINVAL, "rank must be a multiple of 8 up to 128");
+        if (!a || !b || !adapter_of_image) return e->fail(VPE_EINVAL, "null pointer");
+        if ((((uintptr_t)a | (uintptr_t)b) & 15) || ((uintptr_t)scale & 3)) return e->fail(VPE_EINVAL, "a and b must be 16-byte aligned, scale to its elements");
+    }
+    Query& y = h.query;
+    if (!e->host_only) {
+        if (h.ran) HIPCHK(e, hipEventSynchronize(h.last_done));
+        for (auto& g : h.graphs) {
+            if (g) (void)hipGraphExecDestroy(g);       // captured with the adapters there were
+            g = nullptr;
+        }
+        if (adapters) {
+            std::unique_ptr<int32_t[]> of(new (std::nothrow) int32_t[e->T]);
+            if (!of) return e->fail(VPE_ENOMEM, "out of host memory");
+            for (int i = 0; i < e->T; ++i) of[i] = adapter_of_image[i / e->N];
+            HIPCHK(e, hipMemcpy(y.adapter, of.get(), 4 * (size_t)e->T, hipMemcpyHostToDevice));
+        }
+    }
+    y.adapters = adapters; y.rank = rank;
+    y.a = a; y.b = b; y.scale = scale;
     return VPE_OK;
 }
 

@@ -10,7 +10,7 @@ import vpe_inputs as vi
 
 from . import binding as vpe
 
-KIND = {"seg": vi.HEAD_SEG, "depth": vi.HEAD_DEPTH, "det": vi.HEAD_DET, "dpt": vi.HEAD_DPT}
+KIND = {"seg": vi.HEAD_SEG, "depth": vi.HEAD_DEPTH, "det": vi.HEAD_DET, "dpt": vi.HEAD_DPT, "query": vi.HEAD_QUERY}
 
 
 def head_cfgs(spec, seed, kinds, every_n=None):
@@ -22,7 +22,7 @@ def head_cfgs(spec, seed, kinds, every_n=None):
         seen[k] = rep + 1
         hw = vi.make_head_weights(spec, KIND[k], seed + 1000 * rep)
         dicts.append(hw)
-        classes = spec.seg_classes if k == "seg" else spec.det_classes if k == "det" else 0
+        classes = spec.seg_classes if k == "seg" else spec.det_classes if k in ("det", "query") else 0
         cfgs.append(vpe.HeadCfg(kind=KIND[k], weights=vi.pack_head(spec, KIND[k], hw), classes=classes,
                                 channels=0 if k == "seg" else spec.head_ch,
                                 every_n=1 if every_n is None else every_n[i]))

@@ -39,6 +39,7 @@ HEAD_SEG = 0
 HEAD_DEPTH = 1
 HEAD_DET = 2
 HEAD_DPT = 3
+HEAD_QUERY = 4
 
 
 @dataclass(frozen=True)
@@ -208,6 +209,10 @@ def head_layout(spec: ModelSpec, kind: int) -> List[Tuple[str, Tuple[int, ...]]]
                 ("head2_w", (32, F // 2, 3, 3)), ("head2_b", (32,)),
                 ("head3_w", (1, 32)), ("head3_b", (1,))]
         return out
+    if kind == HEAD_QUERY:   # head_ch queries, det_classes classes
+        return [("query", (Ch, D)), ("q_w", (D, D)), ("q_b", (D,)), ("kv_w", (2 * D, D)), ("kv_b", (2 * D,)),
+                ("out_w", (D, D)), ("out_b", (D,)), ("ls1", (D,)), ("norm_g", (D,)), ("norm_b", (D,)),
+                ("cls_w", (spec.det_classes, D)), ("cls_b", (spec.det_classes,))]
     raise ValueError(f"unknown head kind {kind}")
 
 
