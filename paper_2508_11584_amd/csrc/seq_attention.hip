@@ -39,9 +39,25 @@ SeqAttnPlan plan_seq_attention(const vpe_attention_args& a) {
     // workgroup's rows share them.  fp32 waves split every operand that they read: keys shared by four waves of 32 rows are split four times as often.
     int64_t blocks = with_rows(most <= 32 ? 32 : 128);
     if (most > 32 && blocks * plan.sets < 256) blocks = with_rows(a.dtype == VPE_F32 || blocks * plan.sets >= 96 ? 64 : 32);
-    // Parts of at least 256 keys until two workgroups for every CU are there
+    // Parts of the keys where row blocks are few, joined by a second launch.  One launch, for few keys: us on the card / on the host for one and for
+    // two, 6 heads of 64: 257 keys 6.8 / 13.2 and 9.0 / 16.0, 700 8.6 / 13.2 and 9.4 / 16.1, 1370 11.5 / 13.1 and 10.0 / 16.1, 2740 18.0 / 13.1 and
+    // 11.3 / 16.0; 32 of 128: 700 12.4 / 12.6 and 11.9 / 15.5, 1370 17.8 / 12.7 and 12.9 / 15.3; 12 of 64 in fp32: 257 11.7 / 12.4 and 12.5 / 15.0,
+    // 700 18.5 / 12.9 and 13.1 / 15.7.
+    const bool wide = a.dtype == VPE_F32, one = (int64_t)a.max_k * a.head_dim <= (wide ? 24 : 96) << 10;
+    // Workgroups for every CU and no more (a token, 8 key heads of 128, 16384 keys: 12 parts 25.6 us, 32 29.3, 64 42; 16 heads of 64, 12000
+    // keys: 12 19.9, 32 24.8), of 512 keys and up (32 heads of 128, 2740 keys: 18.4, of 256 24.5); fp32, bound by its products, shares 256 keys
+    // and up (a token, 8 heads of 128, 16384 keys: 12 parts 97 us, 32 53, 64 66), with more rows among two workgroups for a CU, which fit then
+    // (ViT-S 476x630: one part 63 us, three 45).  Many sequences are taken to be of many lengths: then up to four for a CU, of 3200 keys and up,
+    // even things out (24 sequences up to 16384, 8 key heads of 128: one part 214 us, 3 154, 5 138, 7 151).  Their number is odd: sets go round the
+    // 8 XCDs, and with 2, 4 or 8 parts an XCD has the first parts, which all sequences have, or the last ones always (the same, 4 parts: 165; 48
+    // sequences up to 14200: 2 parts 313, 3 266, 4 331, 5 263).
     const int64_t base = blocks * plan.sets;
-    plan.splits = base < 256 ? (int)std::max<int64_t>(1, std::min<int64_t>({512 / base, up(a.max_k, 256), 64})) : 1;
+    int64_t parts = std::min<int64_t>({(wide && most > 32 ? 512 : 256) / base, up(a.max_k, wide ? 256 : 512), wide ? 63 : 15});
+    if (a.sequences > 1) {
+        parts = std::max(parts, std::min<int64_t>(1024 / base, a.max_k / 3200));
+        if (parts % 2 == 0 && parts) parts = parts == 2 ? 3 : parts - 1;
+    }
+    plan.splits = one ? 1 : (int)std::max<int64_t>(1, parts);
     plan.per_split = (int)up(up(a.max_k, plan.splits), 128) * 128;
     plan.per_split = std::max(plan.per_split, 128);
     plan.splits = (int)std::max<int64_t>(1, up(a.max_k, plan.per_split));

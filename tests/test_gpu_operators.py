@@ -171,6 +171,19 @@ def test_attention_against_its_definition(form, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ks, heads, kv_heads, head_dim", [
+    ([1537], 3, 1, 64), ([1536], 3, 1, 64), ([769], 2, 2, 128), ([768], 2, 2, 128), ([385, 384, 1], 2, 1, 64),                # one launch and two
+    ([6401, 3, 0, 6400], 4, 2, 64), ([9700, 128, 3233, 3234, 1], 2, 1, 128), ([513] * 70 + [7000], 2, 1, 64), ([1600] * 40, 8, 8, 64)])   # parts of many lengths
+def test_attention_of_tokens_in_parts(ks, heads, kv_heads, head_dim, dtype):
+    gen = torch.Generator().manual_seed(sum(ks))
+    qs = [1 + i % 2 for i in range(len(ks))]
+    q_at, k_at, T = places(qs), places(ks), DTYPES[dtype]
+    q = normal(gen, (q_at[-1] + 2, heads, head_dim), 1.6, T)
+    k, v = (normal(gen, (k_at[-1] + 2, kv_heads, head_dim), 1.6, T) for _ in range(2))
+    check_attention(q, k, v, q_at, ks, k_at, dtype=dtype, causal=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("layout", ["rows_of_qkv", "heads_first", "slots", "broadcast_value"])
 def test_attention_reads_strided_tensors(layout, dtype):
     gen, T = torch.Generator().manual_seed(5), DTYPES[dtype]
