@@ -218,7 +218,8 @@ int vpe_preprocess_u8(const uint8_t* frames, int batch, int src_h, int src_w, fl
  *   the keys, so tight ones are faster.  Offsets that are negative, decreasing or past q_rows / k_rows are cut to the rows there are.
  *   Scores and sums are fp32; bf16 calls round the probabilities to bf16 for the product with v, the sum takes them unrounded.
  * Limits: head_dim 64 or 128, heads a multiple of kv_heads; q, k, v, out 16-byte aligned, their strides (in elements) of rows
- * and heads multiples of 16 bytes and not negative, last axis contiguous, out's at least head_dim. */
+ * and heads multiples of 16 bytes and not negative, last axis contiguous, out's at least head_dim; up to 4096 heads, 2^24 sequences, 2^30 rows,
+ * 2^23 elements from a row of k or v to the next. */
 typedef struct {
     int32_t dtype;                    /* vpe_dtype of q, k, v and out */
     int32_t heads, kv_heads, head_dim;
@@ -275,7 +276,7 @@ int vpe_block_norm(const vpe_block_norm_args* args, void* stream);
  *   together share its reads.  Sums are fp32; bf16 calls carry x A^T to the second product in two bf16 terms (16 bits).
  * Limits: in_features a multiple of 64, rank a multiple of 8 up to 128 (fewer: zero rows and columns do not change the result);
  * x, weight, A and B 16-byte aligned, x's row stride a multiple of 16 bytes and at least in_features; out's row stride at least
- * out_features. */
+ * out_features; up to 2^30 rows, 2^20 in_features, 2^23 out_features. */
 typedef struct {
     int32_t dtype;                    /* vpe_dtype of x, weight, a, b and (out_f32 = 0) out */
     int32_t out_f32;                  /* 1: out is fp32 */
