@@ -8,7 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
-from struct import Struct
+from struct import Struct, error as StructError
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -226,6 +226,13 @@ def _workspace(t, index: int):
     return t.data_ptr(), t.numel()
 
 
+def _pack(form, *values) -> bytes:
+    try:
+        return form.pack(*values)
+    except (StructError, OverflowError) as e:             # (a size that is no integer of its field's width)
+        _refuse(str(e))
+
+
 def _enqueue(call, packed: bytes, index: int, stream) -> None:
     """Makes the call with the tensors' device current; stream: a torch stream, a raw hipStream_t as int, or None (the default stream)."""
     if index < 0:
@@ -296,8 +303,8 @@ def attention(q, k, v, out, *, q_offsets, k_offsets, max_q: int, max_k: int, k_l
     op, o_row, o_head = _heads_matrix("out", out, q_shape, q.dtype, dev)
     ends, each = (sequences + 1,), (sequences,)
     wp, wb = _workspace(workspace, dev)
-    packed = _PACK_ATTENTION.pack(
-        dtype, heads, kv_heads, head_dim, sequences, max_q, max_k, q_rows, k_rows, 1 if causal else 0, head_dim ** -0.5 if scale is None else scale, cap,
+    packed = _pack(
+        _PACK_ATTENTION, dtype, heads, kv_heads, head_dim, sequences, max_q, max_k, q_rows, k_rows, 1 if causal else 0, head_dim ** -0.5 if scale is None else scale, cap,
         qp, kp, vp, op, q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, _ptr("q_offsets", q_offsets, dev, _i32, ends),
         _ptr("k_offsets", k_offsets, dev, _i32, ends), _ptr("k_lengths", k_lengths, dev, _i32, each), _ptr("prefix", prefix, dev, _i32, each),
         _ptr("slopes", slopes, dev, _f32, (heads,)), _ptr("q_coords", q_coords, dev, _f32, (q_rows, 2)),
@@ -334,8 +341,8 @@ def block_norm(x, out, *, branch=None, normed=None, post: int = VPE_NORM_NONE, p
     table = gate if gate is not None else scale if scale is not None else shift
     requests = 0 if table is None else table.shape[0]
     vector, modulation = (dim,), (requests, dim)
-    packed = _PACK_BLOCK_NORM.pack(
-        dtype, rows, dim, requests, post, pre, residual_scale, eps, xp, bp, op, np_, x_row, branch_row, out_row, normed_row,
+    packed = _pack(
+        _PACK_BLOCK_NORM, dtype, rows, dim, requests, post, pre, residual_scale, eps, xp, bp, op, np_, x_row, branch_row, out_row, normed_row,
         _ptr("post_gain", post_gain, dev, _f32, vector), _ptr("post_bias", post_bias, dev, _f32, vector), _ptr("pre_gain", pre_gain, dev, _f32, vector),
         _ptr("pre_bias", pre_bias, dev, _f32, vector), _ptr("layer_scale", layer_scale, dev, _f32, vector), _ptr("gate", gate, dev, _f32, modulation),
         _ptr("scale", scale, dev, _f32, modulation), _ptr("shift", shift, dev, _f32, modulation), _ptr("request", request, dev, _i32, (rows,)))
@@ -379,8 +386,8 @@ def adapter_linear(x, weight, out, *, bias=None, a=None, b=None, adapter=None, s
     xp, x_row = _matrix("x", x, x.shape, t, dev)
     op, out_row = _matrix("out", out, (rows, out_features), _f32 if out_f32 else t, dev)
     wp, wb = _workspace(workspace, dev)
-    packed = _PACK_ADAPTER.pack(
-        dtype, 1 if out_f32 else 0, rows, in_features, out_features, adapters, rank, xp, _ptr("weight", weight, dev, t, weight.shape),
+    packed = _pack(
+        _PACK_ADAPTER, dtype, 1 if out_f32 else 0, rows, in_features, out_features, adapters, rank, xp, _ptr("weight", weight, dev, t, weight.shape),
         _ptr("bias", bias, dev, _f32, (out_features,)), op, x_row, out_row, _ptr("a", a, dev, t, (adapters, rank, in_features)),
         _ptr("b", b, dev, t, (adapters, out_features, rank)), _ptr("adapter", adapter, dev, _i32, (rows,)), _ptr("scale", scale, dev, _f32, (adapters,)), wp, wb)
     _enqueue(lib().vpe_adapter_linear, packed, dev, stream)
@@ -626,9 +633,11 @@ class Engine:
             dtype, dim = _bf16 if self.dtype == VPE_BF16 else _f32, self.cfg.dim
             if a.dim() != 3 or len(adapter_of_image) != self.cfg.batch:
                 _refuse("a must be [adapters, rank, dim], adapter_of_image one index an image")
+            if a.get_device() < 0 and not self.host_only:
+                _refuse("tensors must be in device memory")
             n, rank, device = a.shape[0], a.shape[1], self._ws.get_device() if self._ws is not None else a.get_device()
             ptrs = (_ptr("a", a, device, dtype, (n, rank, dim)), _ptr("b", b, device, dtype, (n, 2 * dim, rank)), _ptr("scale", scale, device, _f32, (n,)))
-            vpe_set_head_adapters(self.handle, head, n, rank, *ptrs, adapter_of_image)
+            vpe_set_head_adapters(self.handle, head, n, rank, *ptrs, [i if 0 <= i < n else -1 for i in adapter_of_image])
         self._adapters[head] = (a, b, scale)
 
     def sync(self) -> None:

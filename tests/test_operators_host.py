@@ -135,3 +135,13 @@ def test_binding_refuses_tensors_that_do_not_fit():
         assert e.value.code == vpe.VPE_EINVAL, n
     # one row or one head: the stride of its axis says nothing
     assert binding._row_stride("x", torch.empty_strided((1, 8), (1, 1))) == 8
+
+
+@pytest.mark.parametrize("over", [dict(max_q=2 ** 40), dict(max_k=2.5), dict(max_q=None), dict(cap=1e300), dict(cap="1")])
+def test_sizes_that_are_no_numbers_of_their_fields_are_refused(over):
+    import torch
+    off, q = torch.tensor([0, 4], dtype=torch.int32), torch.zeros(4, 2, 64)
+    with pytest.raises(vpe.VpeError) as e:
+        vpe.attention(q, q, q, q.clone(), q_offsets=off, k_offsets=off, **{**dict(max_q=4, max_k=4), **over})
+    # (1e300 becomes an infinite float, which the library refuses: here the tensors' memory is refused before)
+    assert e.value.code == vpe.VPE_EINVAL and ("device memory" not in str(e.value) or over.get("cap") == 1e300)

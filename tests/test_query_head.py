@@ -66,6 +66,7 @@ def test_adapters_are_checked():
         eng.set_head_adapters(1, a, b[:, :D], (0, 1))
     with pytest.raises(vpe.VpeError, match="scale"):
         eng.set_head_adapters(1, a, b, (0, 1), scale=torch.ones(3))
+    eng.set_head_adapters(1, a, b, (2 ** 40, -2 ** 40))          # (no index of an adapter: the images have none)
     call = dict(engine=eng.handle, head=1, adapters=2, rank=16, a_ptr=4096, b_ptr=8192, scale_ptr=None, adapter_of_image=(0, 1))
     vpe.vpe_set_head_adapters(**call)
     for over, needle in [(dict(rank=12), "rank"), (dict(rank=0), "rank"), (dict(rank=136), "rank"), (dict(adapters=-1), "negative"), (dict(a_ptr=None), "null"),
