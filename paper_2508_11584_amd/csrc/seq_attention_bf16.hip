@@ -7,9 +7,9 @@ namespace {
 template <bool CAP, int DIST>
 SeqShape of(int head_dim, int rows) {
     // (with these 64 keys at a time take a register or more too many)
-    constexpr int K64 = CAP || DIST == DIST_LINE ? 32 : 64;
+    constexpr int K64 = CAP || DIST == DIST_LINE ? 32 : 64, K128 = CAP && DIST == DIST_GRID ? 32 : 64;
     if (head_dim == 64) return rows == 128 ? seq_shape<bf16, 64, K64, 4, 1, CAP, DIST, 3>() : rows == 64 ? seq_shape<bf16, 64, 32, 2, 2, CAP, DIST, 3>() : seq_shape<bf16, 64, 32, 1, 4, CAP, DIST, 2>();
-    return rows == 128 ? seq_shape<bf16, 128, 64, 4, 1, CAP, DIST, 2>() : rows == 64 ? seq_shape<bf16, 128, 32, 2, 2, CAP, DIST, 2>() : seq_shape<bf16, 128, 32, 1, 4, CAP, DIST, 1>();
+    return rows == 128 ? seq_shape<bf16, 128, K128, 4, 1, CAP, DIST, 2>() : rows == 64 ? seq_shape<bf16, 128, 32, 2, 2, CAP, DIST, 2>() : seq_shape<bf16, 128, 32, 1, 4, CAP, DIST, 1>();
 }
 
 }  // namespace

@@ -261,6 +261,19 @@ def test_attention_with_steep_and_flat_scores(scale, dtype):
     check_attention(q[:1], k, v, [0, 1], [300], [0, 300], dtype=dtype, scale=scale)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("head_dim", [64, 128])
+@pytest.mark.parametrize("slope, spread", [(0.7, 1.0), (4.0, 30.0), (-0.5, 5.0)])
+def test_attention_with_steep_distances(slope, spread, head_dim, dtype):
+    gen, T = torch.Generator().manual_seed(9), DTYPES[dtype]
+    for qs, ks, grid in (([1, 2], [2000, 700], False), ([300], [300], False), ([90, 5], [400, 260], False), ([200, 1], [200, 300], True)):
+        q_at, k_at = places(qs), places(ks)
+        q = normal(gen, (q_at[-1], 2, head_dim), 1.6, T)
+        k, v = (normal(gen, (k_at[-1], 1, head_dim), 1.6, T) for _ in range(2))
+        coords = dict(coords=(normal(gen, (q.shape[0], 2), 10.0 * spread), normal(gen, (k.shape[0], 2), 10.0 * spread))) if grid else {}
+        check_attention(q, k, v, q_at, ks, k_at, dtype=dtype, causal=not grid, slopes=torch.tensor([slope, slope / 8], device="cuda"), **coords)
+
+
 def test_attention_cuts_offsets_that_are_wrong():
     """Offsets past the rows, decreasing or negative ones, and lengths beyond the bounds never leave the tensors."""
     gen = torch.Generator().manual_seed(2)
