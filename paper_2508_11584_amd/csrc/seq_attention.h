@@ -522,13 +522,40 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
     constexpr float MOVE = 1073741824.0f;
     float highest = 0.0f;
     bool all_started = false;
-    auto begin_rows = [&](f32x16 (&sc)[NB]) {
-        float rel = sc[0][0];
+    // Steep scores may pass that within a tile, and attention_row takes a hundred times as long: then the tile's exponents are looked at first.  Scores
+    // are taken to be steep by what a wave sees: distances whose slope may add 48 from its tile to its next (of coordinates nothing is known), 100
+    // between two scores of its first tile, or a probability of 2^60.  (16 tokens of caches up to 7600, slopes up to 0.7: 782 us, 53 so; ViT-B 518x518, scores
+    // of 30 and of 60 nats a standard deviation: 190 and 836, 29 so.  Costs 3 % where it is not needed: on a grid 31.8, 32.8 so.)
+    bool steep = DIST == DIST_GRID || (DIST == DIST_LINE && __any(fabsf(slope2) * (KW * KT) > 48.0f));
+    auto hold = [&](f32x16 (&sc)[NB]) {
+        float top = sc[0][0];
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) rel = fmaxf(rel, sc[b][v]);
+            for (int v = 0; v < 16; ++v) top = fmaxf(top, sc[b][v]);
+        top = exponent(top);
+        if (!__any(top > 64.0f)) return;
+        top = halves_max(top);
+        const float by = top > 30.0f && top < INFINITY ? top : 0.0f;
+        rescale(by, __builtin_amdgcn_exp2f(-by));
+        if constexpr (!PLAIN) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) sc[b][v] -= by;
+        }
+    };
+    auto begin_rows = [&](f32x16 (&sc)[NB]) {
+        float rel = sc[0][0], low = INFINITY;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                rel = fmaxf(rel, sc[b][v]);
+                low = sc[b][v] > -INFINITY && sc[b][v] < low ? sc[b][v] : low;
+            }
         rel = exponent(halves_max(rel));
+        steep = steep || __any(rel - exponent(low) > 100.0f);
         const bool first = !started && rel > -INFINITY;
         const float by = first ? rel : 0.0f;
         m += by;                                          // (the row's sums are zero)
@@ -541,28 +568,10 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
         started = started | first;
         all_started = __all(started | !real);
     };
-    // Distances take a row's scores from tile to tile by more than that, steep ones: then the tile's exponents are looked at first (a step towards
-    // the row, a wave's next tile of KW, may add its width times the slope; of coordinates nothing is known).  Costs 3 % where it is not needed (ViT-B
-    // 518x518 on a grid 31.8 us, 32.8 so); 16 tokens of caches up to 7600, slopes up to 0.7, took 782 us without it, 53 so.
-    const bool steep = DIST == DIST_GRID || (DIST == DIST_LINE && __any(fabsf(slope2) * (KW * KT) > 48.0f));
-    auto hold = [&](f32x16 (&sc)[NB]) {
-        float top = sc[0][0];
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) top = fmaxf(top, sc[b][v]);
-        if (!__any(top > 64.0f)) return;
-        top = halves_max(top);
-        const float by = top > 30.0f && top < INFINITY ? top : 0.0f;
-        rescale(by, __builtin_amdgcn_exp2f(-by));
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) sc[b][v] -= by;
-    };
     auto move_reference = [&] {
         const float top = halves_max(highest);
         const bool grow = top > MOVE;
+        steep = steep || __any(top > 1.15e18f);
         const float by = grow ? __builtin_amdgcn_logf(top) : 0.0f;
         rescale(by, grow ? __builtin_amdgcn_exp2f(-by) : 1.0f);
         highest = 0.0f;
@@ -628,7 +637,7 @@ __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const 
                     if (32 * b + 8 * (v >> 2) + (v & 3) >= left) sc[b][v] = -INFINITY;
         }
         if (!all_started) begin_rows(sc);
-        if (DIST != DIST_NONE && steep) hold(sc);
+        if (steep) hold(sc);
         finish(sc, values, f0);
     };
 

@@ -274,6 +274,18 @@ def test_attention_with_steep_distances(slope, spread, head_dim, dtype):
         check_attention(q, k, v, q_at, ks, k_at, dtype=dtype, causal=not grid, slopes=torch.tensor([slope, slope / 8], device="cuda"), **coords)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nats", [15.0, 60.0, 300.0])
+@pytest.mark.parametrize("kw", [dict(), dict(cap=200.0), dict(causal=True)])
+def test_attention_with_scores_far_apart(nats, kw, dtype):
+    gen, T = torch.Generator().manual_seed(11), DTYPES[dtype]
+    for qs, ks, d in (([1, 2], [2000, 700], 64), ([260], [260], 128), ([700], [700], 64)):
+        q_at, k_at = places(qs), places(ks)
+        q = normal(gen, (q_at[-1], 2, d), nats, T)
+        k, v = (normal(gen, (k_at[-1], 1, d), 1.0, T) for _ in range(2))
+        check_attention(q, k, v, q_at, ks, k_at, dtype=dtype, **kw)
+
+
 def test_attention_cuts_offsets_that_are_wrong():
     """Offsets past the rows, decreasing or negative ones, and lengths beyond the bounds never leave the tensors."""
     gen = torch.Generator().manual_seed(2)
