@@ -267,7 +267,7 @@ constexpr int seq_lds_bytes() {
 // A wave computes scores transposed, S^T = K Q^T: a lane holds half of one row's scores, reductions over the keys stay in the lane but for one
 // exchange, and the probabilities are the second product's operand, O^T = V^T P^T, as they lie.
 // An instantiation per kind of score (with all of them behind run-time branches a tile of slopes alone took twice a plain one's time: ViT-B 518x518 32
-// us, so 25).
+// us, so 28).
 template <typename T, int D, int KT, int QW, int KW, bool CAP, int DIST, int OCC>
 __global__ __launch_bounds__(64 * QW * KW, OCC) void seq_attention_kernel(const vpe_attention_args p, const SeqAttnGrid grid) {
     using M = SeqMma<T, D>;

@@ -31,10 +31,10 @@ SeqAttnPlan plan_seq_attention(const vpe_attention_args& a) {
         return plan.packed ? all : direct;
     };
     // us, workgroups of 128 rows (four waves of 32) / 64 (two, by two that share the keys) / 32 (four that share the keys), by workgroups of 128:
-    //     72  ViT-S 476x630         26 / 23 / 15       176  ViT-L 518x518             33 / 24 / 25      2112  ViT-g 518x518 x 8           126 / 155 / 211
-    //    132  ViT-B 518x518         30 / 23 / 24       264  ViT-B 518x518 x 2         31 / 28 / 37       256  8192 causal, 16 heads of 128  285 / 338 / 615
-    //    132  the same, a grid      36 / 31 / 32       352  ViT-L 518x518 x 2         32 / 30 / 41       410  five views on a grid         58 / 56 / 62
-    //    132  the same, fp32        66 / 75 / 88       192  3000 fp32, 8 heads of 128 184 / 175 / 304
+    //     72  ViT-S 476x630         27 / 22 / 16       176  ViT-L 518x518             27 / 24 / 27      2112  ViT-g 518x518 x 8           133 / 160 / 218
+    //    132  ViT-B 518x518         26 / 23 / 25       264  ViT-B 518x518 x 2         32 / 29 / 39       256  8192 causal, 16 heads of 128  301 / 357 / 708
+    //    132  the same, a grid      46 / 32 / 33       352  ViT-L 518x518 x 2         32 / 31 / 42       410  five views on a grid         60 / 57 / 63
+    //    132  the same, fp32        69 / 74 / 91       192  3000 fp32, 8 heads of 128 194 / 184 / 312
     // Few rows: one launch is as long as its longest workgroup, so the keys are shared by more waves; many: reading the tiles counts, and a
     // workgroup's rows share them.  fp32 waves split every operand that they read: keys shared by four waves of 32 rows are split four times as often.
     int64_t blocks = with_rows(most <= 32 ? 32 : 128);
