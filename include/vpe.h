@@ -147,7 +147,7 @@ typedef struct {
  *                  of class logits, by the operators for packed requests below.  t = query, q = t q_w^T + q_b;
  *                  k, v = the two halves of the map's rows times kv_w^T + kv_b (plus the image's adapter, vpe_set_head_adapters);
  *                  o = attention of q over the image's k and v, dim / 64 heads of 64, scores times 1/8;
- *                  x = t + ls1 (o out_w^T + out_b); logits = LayerNorm(x) cls_w^T + cls_b.
+ *                  x = t + ls1 (o out_w^T + out_b); logits = LayerNorm(x) cls_w^T + cls_b (ln_eps of the backbone).
  *                  weights: query [channels][dim], q_w [dim][dim], q_b [dim], kv_w [2 dim][dim], kv_b, out_w [dim][dim], out_b,
  *                  ls1 [dim], norm_g, norm_b, cls_w [classes][dim], cls_b.
  *                  outputs: 0 = logits fp32 [B][channels][classes].
@@ -436,7 +436,8 @@ int vpe_time_kernel(vpe_engine* e, int which, int reps, float* ms_per_launch, do
 /* Low-rank adapters of a VPE_HEAD_QUERY head's kv projection: image i of a batch has adapter adapter_of_image[i] (HOST array
  * [batch]; outside 0 .. adapters - 1: none).  a [adapters][rank][dim], b [adapters][2 dim][rank] in the engine's dtype and scale
  * [adapters] in fp32 (null: 1) are DEVICE memory as vpe_adapter_linear takes it, read by every later run and to be kept until the
- * next call or vpe_destroy; adapters 0 takes them away.  Blocks until the head's last run has finished; a set-up call. */
+ * next call or vpe_destroy; adapters 0 takes them away.  Blocks until the head's last run has finished; a set-up call, not for the
+ * time in which a graph that the caller captured a run of the head into may run. */
 int vpe_set_head_adapters(vpe_engine* e, int head, int adapters, int rank, const void* a, const void* b, const float* scale,
                           const int32_t* adapter_of_image);
 
