@@ -276,7 +276,7 @@ int vpe_block_norm(const vpe_block_norm_args* args, void* stream);
  *   together share its reads.  Sums are fp32; bf16 calls carry x A^T to the second product in two bf16 terms (16 bits).
  * Limits: in_features a multiple of 64, rank a multiple of 8 up to 128 (fewer: zero rows and columns do not change the result);
  * x, weight, A and B 16-byte aligned, x's row stride a multiple of 16 bytes and at least in_features; out's row stride at least
- * out_features; up to 2^30 rows, 2^20 in_features, 2^23 out_features. */
+ * out_features; up to 2^30 rows, 2^20 in_features, 2^23 out_features, 2^20 elements from a row of x to the next. */
 typedef struct {
     int32_t dtype;                    /* vpe_dtype of x, weight, a, b and (out_f32 = 0) out */
     int32_t out_f32;                  /* 1: out is fp32 */

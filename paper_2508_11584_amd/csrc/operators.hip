@@ -133,6 +133,7 @@ int vpe_adapter_linear(const vpe_adapter_linear_args* args, void* stream) {
     if (a.rows == 0) return VPE_OK;
     if (!a.x || !a.weight || !a.out) REFUSE("null pointer");
     if (a.x_row < a.in_features || a.x_row % (a.dtype == VPE_BF16 ? 8 : 4)) REFUSE("x's row stride must be at least in_features and a multiple of 16 bytes");
+    if (a.rows > 1 && a.x_row > (1 << 20)) REFUSE("x's row stride above 2^20 elements");       // (a tile's offsets are 32-bit)
     if (a.out_row < a.out_features) REFUSE("out's row stride must be at least out_features");
     if (!aligned(a.x, 16) || !aligned(a.weight, 16)) REFUSE("x and weight must be 16-byte aligned");
     if (!aligned(a.out, a.out_f32 || a.dtype == VPE_F32 ? 4 : 2) || !aligned(a.bias, 4)) REFUSE("arrays must be aligned to their elements");

@@ -145,3 +145,8 @@ def test_sizes_that_are_no_numbers_of_their_fields_are_refused(over):
         vpe.attention(q, q, q, q.clone(), q_offsets=off, k_offsets=off, **{**dict(max_q=4, max_k=4), **over})
     # (1e300 becomes an infinite float, which the library refuses: here the tensors' memory is refused before)
     assert e.value.code == vpe.VPE_EINVAL and ("device memory" not in str(e.value) or over.get("cap") == 1e300)
+
+
+def test_rows_of_x_too_far_apart_for_a_tile_are_refused():
+    a = adapter_args(x_row=(1 << 20) + 8)
+    assert vpe.lib().vpe_adapter_linear(C.byref(a), None) == vpe.VPE_EINVAL and "stride" in vpe.vpe_last_error(None)
